@@ -35,6 +35,7 @@ extern "C" {
 /* element types */
 #define HVDX_FLOAT32 0
 #define HVDX_FLOAT16 1
+#define HVDX_BFLOAT16 2 /* rows of the language-model operators; the collectives take the first two */
 
 /* reduction: SUM, or AVERAGE = SUM divided by nranks (paper section 3, the step of
  * the data-parallel recipe that averages the gradients; section 5, the optimizer
@@ -559,6 +560,105 @@ int hvdx_broadcast_tensors_step(const void* const* ptrs, const int64_t* nbytes, 
  */
 int hvdx_fold_allreduce(void* const* bufs, int nranks, int64_t count, int dtype, int op, int compress, void* stream);
 
+/*
+ * Language-model operators: what a data-parallel worker computes on either side of the matrix
+ * products whose weights' gradients the calls above average.  Rows are token positions.  A matrix of rows
+ * is a device pointer and a row stride in elements (>= the row's length; the elements of a
+ * row lie side by side), of dtype HVDX_FLOAT32, HVDX_FLOAT16 or HVDX_BFLOAT16, aligned to its
+ * elements, any alignment else.  Statistics, sums and the results called float are binary32; a result
+ * in the rows' type is rounded to nearest even once.  Index arrays are int64.  0 rows is a no-op.
+ * An output may be the very matrix (pointer and stride) that the comment names; otherwise outputs overlap
+ * neither inputs nor one another (HVDX_ERR_ALIAS).  Device contents are not checked.
+ * Errors: HVDX_ERR_INVALID, HVDX_ERR_ALIAS, HVDX_ERR_WORKSPACE, HVDX_ERR_UNSUPPORTED (a row longer than
+ * the operator takes), HVDX_ERR_HIP.
+ *
+ * hvdx_token_logprobs -- for each row z of `vocab` logits, with p = softmax(scale z): the log probability of
+ * one token, the entropy -sum p log p, and the `top` likeliest tokens with their log probabilities.
+ *   scale          one over the temperature; > 0, finite
+ *   tokens[rows]   a token < 0 is none (its log probability is 0), one >= vocab gives NaN; NULL with logprob
+ *   logprob, entropy [rows]  float, out; NULL where not wanted
+ *   top            0 .. HVDX_MAX_TOP, at most vocab
+ *   top_ids, top_logprobs [rows*top]  out, int64 and float, in descending order of the logits, ties to
+ *                  the lowest index
+ *   stats[rows*4]  float, out, 16-byte aligned: what the gradient takes; NULL where not wanted
+ *   workspace      device memory of hvdx_token_logprobs_workspace_bytes(rows, vocab, top) bytes, 16-byte
+ *                  aligned (NULL for 0); contents afterwards are unspecified
+ * A masked logit is minus infinity or any low value (0 log 0 is 0).  In a row that is minus infinity throughout the
+ * log probabilities are minus infinity, the entropy is 0 and the alternatives are the first tokens; in one that
+ * holds a NaN or plus infinity all of them are NaN and the alternatives -1.
+ *
+ * hvdx_token_logprobs_grad -- grad = d/dz of sum over rows of grad_logprob logprob + grad_entropy entropy
+ * (each [rows] float, or NULL for none), from that call's arguments and stats.  grad may be logits.  A row that is minus
+ * infinity throughout has gradient 0.
+ */
+#define HVDX_MAX_TOP 64
+#define HVDX_MAX_VOCAB ((1LL << 31) - 64)
+size_t hvdx_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int top);
+int hvdx_token_logprobs(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                        const int64_t* tokens, float* logprob, float* entropy, int top, int64_t* top_ids,
+                        float* top_logprobs, float* stats, void* workspace, size_t workspace_bytes, void* stream);
+int hvdx_token_logprobs_grad(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                             const int64_t* tokens, const float* stats, const float* grad_logprob,
+                             const float* grad_entropy, void* grad, int64_t grad_stride, void* stream);
+
+/*
+ * hvdx_distill -- a student's loss against a teacher's alternatives: for each row, p = softmax(scale z) and
+ * the teacher's probabilities q_j of tokens ids[j],
+ *   rest = 1: q_j = exp(teacher[j]); what they leave, q_R = max(0, 1 - sum q), is one more outcome, against
+ *             p_R = the sum of p over the tokens that are not listed;
+ *             loss = sum q_j (log q_j - log p_ids[j]) + q_R (log q_R - log p_R)
+ *   rest = 0: q = softmax of teacher over the entries that are there; loss = sum q_j (log q_j - log p_ids[j])
+ *   ids, teacher [rows*entries]  int64 and float (log probabilities; with rest = 0 any scores); an id < 0 is no
+ *                  entry, one >= vocab makes the row's loss and gradient NaN.  A token listed twice counts with both
+ *                  probabilities, entry by entry
+ *   entries        1 .. HVDX_MAX_TOP
+ *   loss[rows]     float, out (NULL where not wanted).  A row without entries has loss 0 (and gradient 0).  It
+ *                  is infinite where the student gives a token of positive q no probability; a q_R of at
+ *                  most 1e-6 then counts as the rounding of 0
+ *   stats[rows*4]  float, out, 16-byte aligned: what hvdx_distill_grad takes; NULL where not wanted
+ *   grad           out, NULL where not wanted: d/dz of sum over rows of grad_loss[row] loss, of the logits' type, its
+ *                  row stride grad_stride; may be logits.  Takes grad_loss ([rows] float)
+ *   workspace      hvdx_distill_workspace_bytes(rows, vocab) bytes, as above
+ * hvdx_distill_grad -- the gradient alone, from that call's arguments and stats.
+ */
+size_t hvdx_distill_workspace_bytes(int64_t rows, int64_t vocab);
+int hvdx_distill(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                 const int64_t* ids, const float* teacher, int entries, int rest, const float* grad_loss, float* loss,
+                 float* stats, void* grad, int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream);
+int hvdx_distill_grad(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                      const int64_t* ids, const float* teacher, int entries, int rest, const float* stats,
+                      const float* grad_loss, void* grad, int64_t grad_stride, void* stream);
+
+/*
+ * hvdx_residual_norm -- the residual connection from one block to the next with the norms on either side, for
+ * each row of `dim` elements: u = y / rms(y) post, x_out = x + scale gate u, h_out = x_out / rms(x_out) weight,
+ * rms(v) = sqrt(mean v^2 + eps).
+ *   x, y           the stream before the block and the block's output; y NULL: no block (x_out NULL too, post and gate
+ *                  NULL; h_out is x's norm)
+ *   post, weight [dim]  float; post NULL: no norm after the block; weight NULL: 1
+ *   gate           [rows / gate_rows][dim], end to end, of gate_dtype (HVDX_FLOAT32 or dtype): a vector for each run of
+ *                  gate_rows rows (gate_rows = rows: one vector; 1: one each); NULL: 1.  gate_rows divides rows
+ *   x_out, h_out   out, rows end to end, of dtype; NULL where not wanted.  x_out may be x or y, h_out y
+ *   stats[rows*2]  float, out, 8-byte aligned: 1/rms(y) (1 without post) and 1/rms(x_out), before x_out is
+ *                  rounded; NULL where not wanted
+ * hvdx_residual_norm_grad -- from x (that call's x_out), y and stats, and the gradients dx, dh of x_out and h_out
+ * (NULL for none, not both): grad_x (may be dx or dh) and grad_y (may be y, dx or dh) of x and y, rows end to end, of
+ * dtype; grad_weight and grad_post [dim] float; grad_gate as gate.  NULL where not wanted; grad_weight is 0
+ * without dh; grad_y needs y, grad_post needs post, grad_gate needs gate.
+ *   workspace      hvdx_residual_norm_grad_workspace_bytes(rows, dim, gate_rows) bytes, 16-byte aligned
+ * The sums over rows are added in a fixed order: the same inputs give the same bits.
+ */
+#define HVDX_MAX_NORM_DIM 32768
+int hvdx_residual_norm(const void* x, int64_t x_stride, const void* y, int64_t y_stride, int dtype, int64_t rows, int64_t dim,
+                       const float* post, const void* gate, int gate_dtype, int64_t gate_rows, float scale,
+                       const float* weight, float eps, void* x_out, void* h_out, float* stats, void* stream);
+size_t hvdx_residual_norm_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t gate_rows);
+int hvdx_residual_norm_grad(const void* x, int64_t x_stride, const void* y, int64_t y_stride, const void* dx,
+                            int64_t dx_stride, const void* dh, int64_t dh_stride, int dtype, int64_t rows, int64_t dim,
+                            const float* post, const void* gate, int gate_dtype, int64_t gate_rows, float scale,
+                            const float* weight, const float* stats, void* grad_x, void* grad_y, float* grad_weight,
+                            float* grad_post, void* grad_gate, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Workspace bytes hvdx_ring_allreduce needs: 0 unless compressing binary32 data,
  * then nranks * (count rounded up to 128) * 2.  Host only. */
 size_t hvdx_ring_workspace_bytes(int nranks, int64_t count, int dtype, int compress);
@@ -604,6 +704,13 @@ int hvdx_ring_chunk(int64_t count, int nranks, int c, int64_t* start, int64_t* l
 #define HVDX_KERNEL_AG_UNPACK 9 /* replacing step N-2 with copy-out (step = N-2) */
 #define HVDX_KERNEL_RING_SMALL 10  /* hvdx_ring_allreduce(_whole, _small, _noalloc): every step in one launch */
 #define HVDX_KERNEL_CYCLE_SMALL 11 /* hvdx_fuse_cycle, hvdx_fuse_allreduce_small: whole cycles in one launch */
+/* the language-model operators: step = -1, nranks = 0, count = elements of the rows */
+#define HVDX_KERNEL_LOGPROBS 12
+#define HVDX_KERNEL_LOGPROBS_GRAD 13
+#define HVDX_KERNEL_DISTILL 14
+#define HVDX_KERNEL_DISTILL_GRAD 15
+#define HVDX_KERNEL_RESIDUAL_NORM 16
+#define HVDX_KERNEL_RESIDUAL_NORM_GRAD 17
 
 typedef struct hvdx_trace_record {
   int32_t kind;     /* HVDX_KERNEL_* */

@@ -6,6 +6,8 @@ to the HIP runtime torch already loaded (one runtime per process).
     from paper_1802_05799_amd import FusedAllreduce
     ar = FusedAllreduce(per_rank_grads, op="average")   # plan + buffers, once
     ar()                                                  # reduce in place
+
+and, for the language models whose gradients it averages, TokenLogprobs, DistillLoss and ResidualNorm (lm.py).
 """
 import operator
 
@@ -13,6 +15,7 @@ import torch  # noqa: F401  (must precede the library load)
 
 from ._lib import (  # noqa: F401
     AVERAGE,
+    BFLOAT16,
     COMPRESS_FP16,
     COMPRESS_NONE,
     DEFAULT_FUSION_ALIGN,
@@ -25,7 +28,10 @@ from ._lib import (  # noqa: F401
     FLOAT16,
     FLOAT32,
     LIB_PATH,
+    MAX_NORM_DIM,
     MAX_RANKS,
+    MAX_TOP,
+    MAX_VOCAB,
     OK,
     PHASE_ALLGATHER,
     PHASE_REDUCE_SCATTER,
@@ -43,6 +49,9 @@ from ._lib import (  # noqa: F401
     hvdx_broadcast_tensors,
     hvdx_broadcast_tensors_placed,
     hvdx_broadcast_tensors_step,
+    hvdx_distill,
+    hvdx_distill_grad,
+    hvdx_distill_workspace_bytes,
     hvdx_fold_allreduce,
     hvdx_fuse_ag_unpack,
     hvdx_fuse_allreduce,
@@ -71,12 +80,19 @@ from ._lib import (  # noqa: F401
     hvdx_ring_reduce_scatter,
     hvdx_ring_step,
     hvdx_ring_workspace_bytes,
+    hvdx_residual_norm,
+    hvdx_residual_norm_grad,
+    hvdx_residual_norm_grad_workspace_bytes,
     hvdx_strerror,
     hvdx_timeline_begin,
     hvdx_timeline_end,
+    hvdx_token_logprobs,
+    hvdx_token_logprobs_grad,
+    hvdx_token_logprobs_workspace_bytes,
     hvdx_version,
 )
 from .cycle import FusedAllreduce, current_stream  # noqa: F401
+from .lm import DistillLoss, ResidualNorm, TokenLogprobs  # noqa: F401
 from .timeline import Timeline  # noqa: F401
 
 

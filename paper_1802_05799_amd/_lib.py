@@ -13,13 +13,14 @@ import os
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libhvdx.so")  # the library build() makes, next to this file
 
-FLOAT32, FLOAT16 = 0, 1
+FLOAT32, FLOAT16, BFLOAT16 = 0, 1, 2  # BFLOAT16: the language-model operators' rows only
 SUM, AVERAGE = 0, 1
 COMPRESS_NONE, COMPRESS_FP16 = 0, 1
 PHASE_REDUCE_SCATTER, PHASE_ALLGATHER = 0, 1
 COPY_IN, COPY_OUT = 0, 1
 OK, ERR_INVALID, ERR_ALIAS, ERR_WORKSPACE, ERR_HIP, ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 MAX_RANKS = 128
+MAX_TOP, MAX_VOCAB, MAX_NORM_DIM = 64, (1 << 31) - 64, 32768  # HVDX_MAX_*
 DEFAULT_FUSION_THRESHOLD = 64 << 20
 DEFAULT_FUSION_ALIGN = 16
 SMALL_BUCKET_BYTES = 4 << 20  # HVDX_SMALL_BUCKET_BYTES
@@ -28,6 +29,7 @@ _p = ctypes.c_void_p
 _i = ctypes.c_int
 _i64 = ctypes.c_int64
 _sz = ctypes.c_size_t
+_f = ctypes.c_float
 _pp = ctypes.POINTER(ctypes.c_void_p)
 _pi64 = ctypes.POINTER(ctypes.c_int64)
 _pi32 = ctypes.POINTER(ctypes.c_int32)
@@ -67,6 +69,16 @@ _SIGNATURES = {
     "hvdx_broadcast_tensors_placed": (_i, [_p, _p, _p, _i, _i64, _i64, _i, _i, _p]),
     "hvdx_broadcast_tensors_step": (_i, [_p, _p, _p, _i, _i64, _i, _i, _i, _p]),
     "hvdx_fold_allreduce": (_i, [_pp, _i, _i64, _i, _i, _i, _p]),
+    "hvdx_token_logprobs_workspace_bytes": (_sz, [_i64, _i64, _i]),
+    "hvdx_token_logprobs": (_i, [_p, _i64, _i, _i64, _i64, _f, _p, _p, _p, _i, _p, _p, _p, _p, _sz, _p]),
+    "hvdx_token_logprobs_grad": (_i, [_p, _i64, _i, _i64, _i64, _f, _p, _p, _p, _p, _p, _i64, _p]),
+    "hvdx_distill_workspace_bytes": (_sz, [_i64, _i64]),
+    "hvdx_distill": (_i, [_p, _i64, _i, _i64, _i64, _f, _p, _p, _i, _i, _p, _p, _p, _p, _i64, _p, _sz, _p]),
+    "hvdx_distill_grad": (_i, [_p, _i64, _i, _i64, _i64, _f, _p, _p, _i, _i, _p, _p, _p, _i64, _p]),
+    "hvdx_residual_norm": (_i, [_p, _i64, _p, _i64, _i, _i64, _i64, _p, _p, _i, _i64, _f, _p, _f, _p, _p, _p, _p]),
+    "hvdx_residual_norm_grad_workspace_bytes": (_sz, [_i64, _i64, _i64]),
+    "hvdx_residual_norm_grad": (_i, [_p, _i64, _p, _i64, _p, _i64, _p, _i64, _i, _i64, _i64, _p, _p, _i, _i64, _f, _p, _p, _p,
+                                     _p, _p, _p, _p, _p, _sz, _p]),
     "hvdx_timeline_begin": (_i, [_i, _i]),
     "hvdx_timeline_end": (_i, [_p, _i, ctypes.POINTER(ctypes.c_int), ctypes.POINTER(ctypes.c_int)]),
 }
@@ -75,6 +87,8 @@ KERNEL_PACK, KERNEL_REDUCE_SCATTER, KERNEL_ALLGATHER, KERNEL_UNPACK, KERNEL_ROUN
 KERNEL_BROADCAST, KERNEL_RS_AG, KERNEL_FOLD = 5, 6, 7
 KERNEL_PACK_RS, KERNEL_AG_UNPACK = 8, 9
 KERNEL_RING_SMALL, KERNEL_CYCLE_SMALL = 10, 11
+KERNEL_LOGPROBS, KERNEL_LOGPROBS_GRAD, KERNEL_DISTILL, KERNEL_DISTILL_GRAD = 12, 13, 14, 15
+KERNEL_RESIDUAL_NORM, KERNEL_RESIDUAL_NORM_GRAD = 16, 17
 TILED_BUFFERS, TILED_REPLACE_IN_TENSORS, TILED_ADD_FROM_TENSORS = 0, 1, 2
 TILED_MAX_BUCKETS, TILED_MAX_BUFFERS = 4, 256  # buckets per call; buckets x ranks in the tensor modes
 
@@ -437,3 +451,43 @@ def hvdx_broadcast_tensors_step(ptrs_dev: int, nbytes_dev: int, voffset_dev: int
                                 nranks: int, root: int, step: int, stream: int = 0) -> None:
     _check(lib.hvdx_broadcast_tensors_step(ptrs_dev, nbytes_dev, voffset_dev, ntensors, total_bytes, nranks, root,
                                            step, stream))
+
+
+# The language-model operators: addresses (0 for NULL) and numbers in the order of include/hvdx.h, the
+# stream last.
+
+
+def hvdx_token_logprobs_workspace_bytes(rows: int, vocab: int, top: int) -> int:
+    return lib.hvdx_token_logprobs_workspace_bytes(rows, vocab, top)
+
+
+def hvdx_token_logprobs(*args) -> None:
+    _check(lib.hvdx_token_logprobs(*args))
+
+
+def hvdx_token_logprobs_grad(*args) -> None:
+    _check(lib.hvdx_token_logprobs_grad(*args))
+
+
+def hvdx_distill_workspace_bytes(rows: int, vocab: int) -> int:
+    return lib.hvdx_distill_workspace_bytes(rows, vocab)
+
+
+def hvdx_distill(*args) -> None:
+    _check(lib.hvdx_distill(*args))
+
+
+def hvdx_distill_grad(*args) -> None:
+    _check(lib.hvdx_distill_grad(*args))
+
+
+def hvdx_residual_norm(*args) -> None:
+    _check(lib.hvdx_residual_norm(*args))
+
+
+def hvdx_residual_norm_grad_workspace_bytes(rows: int, dim: int, gate_rows: int) -> int:
+    return lib.hvdx_residual_norm_grad_workspace_bytes(rows, dim, gate_rows)
+
+
+def hvdx_residual_norm_grad(*args) -> None:
+    _check(lib.hvdx_residual_norm_grad(*args))

@@ -45,68 +45,55 @@ hvdx::LaunchEvents& hvdx::pending_launch_events() {
   return ev;
 }
 
-namespace {
-
-// Times kernel launches for the timeline when it records at this granularity.  A
-// launch record (per-launch mode) hands its events to the one launch in its scope,
-// which stamps them with the kernel's own start and end; a phase record (per-phase
-// mode) covers several launches with event records in the stream before and after.
-class TimedLaunch {
- public:
-  TimedLaunch(int kind, int step, int nranks, int dtype, int compress, int64_t count, hipStream_t st, int root = -1,
-              bool phase = false, int launches = 1)
-      : st_(st), lock_(timeline().mu) {
-    Timeline& t = timeline();
-    if (!t.on || t.per_phase != phase) return;
-    // Launches recorded into a HIP graph run later, at each replay: they get no record.
-    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(st_, &cs) != hipSuccess || cs != hipStreamCaptureStatusNone) return;
-    if ((int)t.entries.size() >= t.capacity) {
-      ++t.dropped;
-      return;
-    }
-    TimelineEntry e{};
-    e.rec.kind = kind;
-    e.rec.step = step;
-    e.rec.launches = launches;
-    e.rec.nranks = nranks;
-    e.rec.dtype = dtype;
-    e.rec.compress = compress;
-    e.rec.root = root;
-    e.rec.count = count;
-    e.start = t.pool[2 * t.entries.size()];
-    e.end = t.pool[2 * t.entries.size() + 1];
-    if (!phase) {
-      t.entries.push_back(e);
-      hvdx::pending_launch_events() = {e.start, e.end};
-      start_ = e.start;
-      end_ = e.end;
-    } else if (hipEventRecord(e.start, st_) == hipSuccess) {
-      t.entries.push_back(e);
-      end_ = e.end;
-    }
+hvdx::TimedLaunch::TimedLaunch(int kind, int step, int nranks, int dtype, int compress, int64_t count, hipStream_t st,
+                               int root, bool phase, int launches)
+    : st_(st), lock_(timeline().mu) {
+  Timeline& t = timeline();
+  if (!t.on || t.per_phase != phase) return;
+  // Launches recorded into a HIP graph run later, at each replay: they get no record.
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(st_, &cs) != hipSuccess || cs != hipStreamCaptureStatusNone) return;
+  if ((int)t.entries.size() >= t.capacity) {
+    ++t.dropped;
+    return;
   }
-  // The lock is still held here: no other thread's launch lands inside the record.
-  ~TimedLaunch() {
-    if (start_) {
-      hvdx::LaunchEvents& ev = hvdx::pending_launch_events();
-      if (ev.start == start_) {  // nothing was launched (an error): a zero-length record
-        ev = hvdx::LaunchEvents{};
-        (void)hipEventRecord(start_, st_);
-        (void)hipEventRecord(end_, st_);
-      }
-      return;
-    }
-    if (end_) (void)hipEventRecord(end_, st_);
+  TimelineEntry e{};
+  e.rec.kind = kind;
+  e.rec.step = step;
+  e.rec.launches = launches;
+  e.rec.nranks = nranks;
+  e.rec.dtype = dtype;
+  e.rec.compress = compress;
+  e.rec.root = root;
+  e.rec.count = count;
+  e.start = t.pool[2 * t.entries.size()];
+  e.end = t.pool[2 * t.entries.size() + 1];
+  if (!phase) {
+    t.entries.push_back(e);
+    pending_launch_events() = {e.start, e.end};
+    start_ = e.start;
+    end_ = e.end;
+  } else if (hipEventRecord(e.start, st_) == hipSuccess) {
+    t.entries.push_back(e);
+    end_ = e.end;
   }
+}
 
- private:
-  hipStream_t st_;
-  std::unique_lock<std::recursive_mutex> lock_;
-  hipEvent_t start_ = nullptr, end_ = nullptr;
-};
+// The lock is still held here: no other thread's launch lands inside the record.
+hvdx::TimedLaunch::~TimedLaunch() {
+  if (start_) {
+    LaunchEvents& ev = pending_launch_events();
+    if (ev.start == start_) {  // nothing was launched (an error): a zero-length record
+      ev = LaunchEvents{};
+      (void)hipEventRecord(start_, st_);
+      (void)hipEventRecord(end_, st_);
+    }
+    return;
+  }
+  if (end_) (void)hipEventRecord(end_, st_);
+}
 
-int fail(int code, const char* fmt, ...) {
+int hvdx::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
@@ -114,9 +101,15 @@ int fail(int code, const char* fmt, ...) {
   return code;
 }
 
-int hip_fail(hipError_t e, const char* what) {
+int hvdx::hip_fail(hipError_t e, const char* what) {
   return fail(HVDX_ERR_HIP, "%s: %s (%s)", what, hipGetErrorName(e), hipGetErrorString(e));
 }
+
+namespace {
+
+using hvdx::fail;
+using hvdx::hip_fail;
+using hvdx::TimedLaunch;
 
 int elem_size(int dtype) {
   switch (dtype) {

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "hvdx.h"
 
 namespace hvdx {
@@ -17,6 +19,26 @@ struct LaunchEvents {
   hipEvent_t start = nullptr, stop = nullptr;
 };
 LaunchEvents& pending_launch_events();
+
+// Records the calling thread's last error (hvdx_last_error) and returns its code.
+int fail(int code, const char* fmt, ...);
+int hip_fail(hipError_t e, const char* what);
+
+// Times kernel launches for the timeline when it records at this granularity.  A
+// launch record (per-launch mode) hands its events to the one launch in its scope,
+// which stamps them with the kernel's own start and end; a phase record (per-phase
+// mode) covers several launches with event records in the stream before and after.
+class TimedLaunch {
+ public:
+  TimedLaunch(int kind, int step, int nranks, int dtype, int compress, int64_t count, hipStream_t st, int root = -1,
+              bool phase = false, int launches = 1);
+  ~TimedLaunch();
+
+ private:
+  hipStream_t st_;
+  std::unique_lock<std::recursive_mutex> lock_;
+  hipEvent_t start_ = nullptr, end_ = nullptr;
+};
 
 // Every rank's base pointer travels in the kernel arguments (1 KiB).
 struct RankPtrs {
@@ -223,6 +245,90 @@ hipError_t launch_pack(const void* const* srcs, const int64_t* numel, const int6
 hipError_t launch_unpack(const RankPtrs& bufs, int64_t count, int buf_dtype, void* const* dsts,
                          const int64_t* numel, const int64_t* offset, int ntensors, int dst_dtype, int nranks,
                          bool ring, hipStream_t stream);
+
+// The language-model operators (vocab_kernels.hip, norm_kernels.hip).  Arguments are validated;
+// strides are in elements.
+struct LogprobArgs {
+  const void* logits;
+  int64_t stride, rows;
+  int vocab;
+  float scale;
+  const int64_t* tokens;
+  float *logprob, *entropy;
+  int top;
+  int64_t* top_ids;
+  float* top_logprobs;
+  float4* stats;  // row's maximum, log of its sum, entropy
+};
+hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream);
+struct LogprobGradArgs {
+  const void* logits;
+  int64_t stride, rows;
+  int vocab;
+  float scale;
+  const int64_t* tokens;
+  const float4* stats;
+  const float *grad_logprob, *grad_entropy;
+  void* grad;
+  int64_t grad_stride;
+};
+hipError_t launch_logprobs_grad(const LogprobGradArgs& g, int dtype, hipStream_t stream);
+struct DistillArgs {
+  const void* logits;
+  int64_t stride, rows;
+  int vocab;
+  float scale;
+  const int64_t* ids;
+  const float* teacher;
+  int entries, rest;
+  const float* grad_loss;
+  float* loss;
+  float4* stats;  // maximum of what the sum is over, its gradient's factor, the row's maximum and log of its sum
+  void* grad;
+  int64_t grad_stride;
+};
+hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream);
+hipError_t launch_distill_grad(const DistillArgs& g, int dtype, hipStream_t stream);
+
+struct NormArgs {
+  const void *x, *y;
+  int64_t x_stride, y_stride, rows;
+  int dim;
+  const float* post;
+  const void* gate;
+  int gate_f32;
+  int64_t gate_rows;
+  float scale, eps;
+  const float* weight;
+  void *x_out, *h_out;  // rows end to end
+  float2* stats;        // the norms' factors: of y (1 without its norm), of x_out
+};
+hipError_t launch_norm(const NormArgs& g, int dtype, hipStream_t stream);
+// How a backward pass's rows are dealt out: `groups` of `span` rows share a vector of the gate; a block has
+// one of a group's `segments`, of `seg_rows` rows, or (one segment) `per_block` whole groups.
+struct NormPlan {
+  int64_t groups, span, segments, seg_rows, per_block, blocks;
+};
+NormPlan norm_plan(int64_t rows, int64_t gate_rows);
+struct NormGradArgs {
+  const void *x, *y, *dx, *dh;
+  int64_t x_stride, y_stride, dx_stride, dh_stride, rows;
+  int dim;
+  const float* post;
+  const void* gate;
+  int gate_f32;
+  int64_t gate_rows;
+  float scale;
+  const float* weight;
+  const float2* stats;
+  void *grad_x, *grad_y;
+  float *grad_weight, *grad_post;
+  void* grad_gate;
+  float* partial;  // blocks x dim for each of weight, post, and gate with more than one segment
+  NormPlan plan;
+};
+hipError_t launch_norm_grad(const NormGradArgs& g, int dtype, hipStream_t stream);
+hipError_t launch_norm_grad_sums(const NormGradArgs& g, int dtype, hipStream_t stream);
 
 }  // namespace hvdx
 

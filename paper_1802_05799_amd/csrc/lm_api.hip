@@ -1,0 +1,329 @@
+// C-ABI of the language-model operators: argument checks, then the launches.  Every check runs before
+// the first HIP call.
+
+#include <math.h>
+
+#include "internal.hpp"
+
+namespace {
+
+using hvdx::fail;
+using hvdx::hip_fail;
+using hvdx::TimedLaunch;
+
+constexpr int64_t kMostRows = 1LL << 31;
+
+int row_elem_size(int dtype) {
+  switch (dtype) {
+    case HVDX_FLOAT32: return 4;
+    case HVDX_FLOAT16:
+    case HVDX_BFLOAT16: return 2;
+    default: return 0;
+  }
+}
+
+// A buffer of a call: what it is called, where it is, and for a matrix its row stride in bytes.
+struct Buffer {
+  const char* name;
+  const void* p;
+  int64_t bytes;
+  int64_t stride;
+  int align;
+};
+
+Buffer vec(const char* name, const void* p, int64_t count, int size, int align = 0) {
+  return {name, p, count * size, 0, align ? align : size};
+}
+Buffer matrix(const char* name, const void* p, int64_t rows, int64_t length, int64_t stride, int size) {
+  return {name, p, ((rows - 1) * stride + length) * size, stride * size, size};
+}
+
+int check_aligned(const Buffer& b, const char* what) {
+  if (reinterpret_cast<uintptr_t>(b.p) % b.align) return fail(HVDX_ERR_INVALID, "%s: %s is not aligned to %d bytes", what, b.name, b.align);
+  return HVDX_OK;
+}
+
+bool meet(const Buffer& a, const Buffer& b) {
+  if (!a.p || !b.p || a.bytes <= 0 || b.bytes <= 0) return false;
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+  return p < q + (uintptr_t)b.bytes && q < p + (uintptr_t)a.bytes;
+}
+
+// Every buffer aligned; no output meets another output, or an input unless it is that very matrix and may be
+// (`same[o]`: a mask over the inputs).
+int check_buffers(const Buffer* in, int nin, const Buffer* out, int nout, const unsigned* same, const char* what) {
+  for (int i = 0; i < nin; ++i)
+    if (int rc = check_aligned(in[i], what)) return rc;
+  for (int o = 0; o < nout; ++o) {
+    if (int rc = check_aligned(out[o], what)) return rc;
+    for (int i = 0; i < nin; ++i) {
+      if (!meet(out[o], in[i])) continue;
+      if (same[o] >> i & 1 && out[o].p == in[i].p && out[o].stride == in[i].stride) continue;
+      return fail(HVDX_ERR_ALIAS, "%s: %s overlaps %s", what, out[o].name, in[i].name);
+    }
+    for (int i = 0; i < o; ++i)
+      if (meet(out[o], out[i])) return fail(HVDX_ERR_ALIAS, "%s: %s overlaps %s", what, out[o].name, out[i].name);
+  }
+  return HVDX_OK;
+}
+
+int check_rows(int64_t rows, int64_t length, int64_t most, int dtype, const char* unit, const char* what) {
+  if (!row_elem_size(dtype)) return fail(HVDX_ERR_INVALID, "%s: unknown dtype %d", what, dtype);
+  if (rows < 0 || rows > kMostRows) return fail(HVDX_ERR_INVALID, "%s: %lld rows outside 0..2^31", what, (long long)rows);
+  if (length < 1) return fail(HVDX_ERR_INVALID, "%s: %s %lld is less than 1", what, unit, (long long)length);
+  if (length > most)
+    return fail(HVDX_ERR_UNSUPPORTED, "%s: %s %lld is more than %lld", what, unit, (long long)length, (long long)most);
+  return HVDX_OK;
+}
+
+int check_stride(const char* name, int64_t stride, int64_t length, int64_t rows, const char* what) {
+  if (rows > 1 && (stride < length || stride > (INT64_MAX >> 4) / rows))
+    return fail(HVDX_ERR_INVALID, "%s: %s's row stride %lld does not fit rows of %lld", what, name, (long long)stride,
+                (long long)length);
+  return HVDX_OK;
+}
+
+int check_scale(float scale, const char* what) {
+  return scale > 0.f && isfinite(scale) ? HVDX_OK : fail(HVDX_ERR_INVALID, "%s: scale %g is not positive and finite", what, scale);
+}
+
+int check_workspace(const void* workspace, size_t given, size_t need, const char* what) {
+  if (!need) return HVDX_OK;
+  if (!workspace || given < need)
+    return fail(HVDX_ERR_WORKSPACE, "%s: workspace of %zu bytes given, %zu needed", what, workspace ? given : (size_t)0, need);
+  if (reinterpret_cast<uintptr_t>(workspace) & 15) return fail(HVDX_ERR_WORKSPACE, "%s: workspace is not 16-byte aligned", what);
+  return HVDX_OK;
+}
+
+int launched(hipError_t e, const char* what) { return e == hipSuccess ? HVDX_OK : hip_fail(e, what); }
+
+// One launch with its record, inside its call's phase record.
+template <typename F>
+hipError_t timed(int kind, int dtype, int64_t count, hipStream_t st, F launch) {
+  TimedLaunch record(kind, -1, 0, dtype, HVDX_COMPRESS_NONE, count, st);
+  return launch();
+}
+
+int check_distill(int64_t rows, int64_t vocab, int dtype, int64_t stride, float scale, int entries, int rest,
+                  const int64_t* ids, const float* teacher, const char* what) {
+  if (int rc = check_rows(rows, vocab, HVDX_MAX_VOCAB, dtype, "vocabulary", what)) return rc;
+  if (int rc = check_stride("logits", stride, vocab, rows, what)) return rc;
+  if (int rc = check_scale(scale, what)) return rc;
+  if (entries < 1 || entries > HVDX_MAX_TOP) return fail(HVDX_ERR_INVALID, "%s: %d entries outside 1..%d", what, entries, HVDX_MAX_TOP);
+  if (rest != 0 && rest != 1) return fail(HVDX_ERR_INVALID, "%s: rest is %d, neither 0 nor 1", what, rest);
+  if (rows > 0 && (!ids || !teacher)) return fail(HVDX_ERR_INVALID, "%s: ids or teacher is NULL", what);
+  return HVDX_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t hvdx_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int top) {
+  (void)rows, (void)vocab, (void)top;
+  return 0;
+}
+
+int hvdx_token_logprobs(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                        const int64_t* tokens, float* logprob, float* entropy, int top, int64_t* top_ids,
+                        float* top_logprobs, float* stats, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* what = "hvdx_token_logprobs";
+  if (int rc = check_rows(rows, vocab, HVDX_MAX_VOCAB, dtype, "vocabulary", what)) return rc;
+  if (int rc = check_stride("logits", stride, vocab, rows, what)) return rc;
+  if (int rc = check_scale(scale, what)) return rc;
+  if (top < 0 || top > HVDX_MAX_TOP || top > vocab)
+    return fail(HVDX_ERR_INVALID, "%s: top %d outside 0..%d or more than the vocabulary", what, top, HVDX_MAX_TOP);
+  if (rows == 0) return HVDX_OK;
+  if (!logits) return fail(HVDX_ERR_INVALID, "%s: logits is NULL", what);
+  if (logprob && !tokens) return fail(HVDX_ERR_INVALID, "%s: logprob needs tokens", what);
+  if (top && (!top_ids || !top_logprobs)) return fail(HVDX_ERR_INVALID, "%s: top_ids or top_logprobs is NULL", what);
+  const size_t need = hvdx_token_logprobs_workspace_bytes(rows, vocab, top);
+  if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
+  const Buffer in[] = {matrix("logits", logits, rows, vocab, stride, row_elem_size(dtype)), vec("tokens", tokens, rows, 8)};
+  const Buffer out[] = {vec("logprob", logprob, rows, 4), vec("entropy", entropy, rows, 4), vec("top_ids", top_ids, rows * top, 8),
+                        vec("top_logprobs", top_logprobs, rows * top, 4), vec("stats", stats, rows * 4, 4, 16),
+                        vec("workspace", workspace, (int64_t)need, 1)};
+  const unsigned same[6] = {};
+  if (int rc = check_buffers(in, 2, out, 6, same, what)) return rc;
+  const hvdx::LogprobArgs g{logits, stride, rows, (int)vocab, scale, tokens, logprob, entropy, top, top_ids, top_logprobs,
+                            reinterpret_cast<float4*>(stats)};
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch phase(HVDX_KERNEL_LOGPROBS, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
+  return launched(timed(HVDX_KERNEL_LOGPROBS, dtype, rows * vocab, st, [&] { return hvdx::launch_logprobs(g, dtype, st); }), what);
+}
+
+int hvdx_token_logprobs_grad(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                             const int64_t* tokens, const float* stats, const float* grad_logprob,
+                             const float* grad_entropy, void* grad, int64_t grad_stride, void* stream) {
+  static const char* what = "hvdx_token_logprobs_grad";
+  if (int rc = check_rows(rows, vocab, HVDX_MAX_VOCAB, dtype, "vocabulary", what)) return rc;
+  if (int rc = check_stride("logits", stride, vocab, rows, what)) return rc;
+  if (int rc = check_stride("grad", grad_stride, vocab, rows, what)) return rc;
+  if (int rc = check_scale(scale, what)) return rc;
+  if (rows == 0) return HVDX_OK;
+  if (!logits || !stats || !grad) return fail(HVDX_ERR_INVALID, "%s: logits, stats or grad is NULL", what);
+  if (grad_logprob && !tokens) return fail(HVDX_ERR_INVALID, "%s: grad_logprob needs tokens", what);
+  const int es = row_elem_size(dtype);
+  const Buffer in[] = {matrix("logits", logits, rows, vocab, stride, es), vec("tokens", tokens, rows, 8),
+                       vec("stats", stats, rows * 4, 4, 16), vec("grad_logprob", grad_logprob, rows, 4),
+                       vec("grad_entropy", grad_entropy, rows, 4)};
+  const Buffer out[] = {matrix("grad", grad, rows, vocab, grad_stride, es)};
+  const unsigned same[1] = {1};
+  if (int rc = check_buffers(in, 5, out, 1, same, what)) return rc;
+  const hvdx::LogprobGradArgs g{logits, stride, rows, (int)vocab, scale, tokens, reinterpret_cast<const float4*>(stats),
+                                grad_logprob, grad_entropy, grad, grad_stride};
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch phase(HVDX_KERNEL_LOGPROBS_GRAD, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
+  return launched(timed(HVDX_KERNEL_LOGPROBS_GRAD, dtype, rows * vocab, st, [&] { return hvdx::launch_logprobs_grad(g, dtype, st); }),
+                  what);
+}
+
+size_t hvdx_distill_workspace_bytes(int64_t rows, int64_t vocab) {
+  (void)rows, (void)vocab;
+  return 0;
+}
+
+int hvdx_distill(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                 const int64_t* ids, const float* teacher, int entries, int rest, const float* grad_loss, float* loss,
+                 float* stats, void* grad, int64_t grad_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* what = "hvdx_distill";
+  if (int rc = check_distill(rows, vocab, dtype, stride, scale, entries, rest, ids, teacher, what)) return rc;
+  if (grad)
+    if (int rc = check_stride("grad", grad_stride, vocab, rows, what)) return rc;
+  if (rows == 0) return HVDX_OK;
+  if (!logits) return fail(HVDX_ERR_INVALID, "%s: logits is NULL", what);
+  if (grad && !grad_loss) return fail(HVDX_ERR_INVALID, "%s: grad needs grad_loss", what);
+  const size_t need = hvdx_distill_workspace_bytes(rows, vocab);
+  if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
+  const int es = row_elem_size(dtype);
+  const Buffer in[] = {matrix("logits", logits, rows, vocab, stride, es), vec("ids", ids, rows * entries, 8),
+                       vec("teacher", teacher, rows * entries, 4), vec("grad_loss", grad_loss, rows, 4)};
+  const Buffer out[] = {matrix("grad", grad, rows, vocab, grad_stride, es), vec("loss", loss, rows, 4),
+                        vec("stats", stats, rows * 4, 4, 16), vec("workspace", workspace, (int64_t)need, 1)};
+  const unsigned same[4] = {1, 0, 0, 0};
+  if (int rc = check_buffers(in, 4, out, 4, same, what)) return rc;
+  const hvdx::DistillArgs g{logits, stride, rows, (int)vocab, scale, ids, teacher, entries, rest, grad_loss, loss,
+                            reinterpret_cast<float4*>(stats), grad, grad_stride};
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch phase(HVDX_KERNEL_DISTILL, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
+  return launched(timed(HVDX_KERNEL_DISTILL, dtype, rows * vocab, st, [&] { return hvdx::launch_distill(g, dtype, st); }), what);
+}
+
+int hvdx_distill_grad(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
+                      const int64_t* ids, const float* teacher, int entries, int rest, const float* stats,
+                      const float* grad_loss, void* grad, int64_t grad_stride, void* stream) {
+  static const char* what = "hvdx_distill_grad";
+  if (int rc = check_distill(rows, vocab, dtype, stride, scale, entries, rest, ids, teacher, what)) return rc;
+  if (int rc = check_stride("grad", grad_stride, vocab, rows, what)) return rc;
+  if (rows == 0) return HVDX_OK;
+  if (!logits || !stats || !grad || !grad_loss)
+    return fail(HVDX_ERR_INVALID, "%s: logits, stats, grad_loss or grad is NULL", what);
+  const int es = row_elem_size(dtype);
+  const Buffer in[] = {matrix("logits", logits, rows, vocab, stride, es), vec("ids", ids, rows * entries, 8),
+                       vec("teacher", teacher, rows * entries, 4), vec("grad_loss", grad_loss, rows, 4),
+                       vec("stats", stats, rows * 4, 4, 16)};
+  const Buffer out[] = {matrix("grad", grad, rows, vocab, grad_stride, es)};
+  const unsigned same[1] = {1};
+  if (int rc = check_buffers(in, 5, out, 1, same, what)) return rc;
+  const hvdx::DistillArgs g{logits, stride, rows, (int)vocab, scale, ids, teacher, entries, rest, grad_loss, nullptr,
+                            const_cast<float4*>(reinterpret_cast<const float4*>(stats)), grad, grad_stride};
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch phase(HVDX_KERNEL_DISTILL_GRAD, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
+  return launched(timed(HVDX_KERNEL_DISTILL_GRAD, dtype, rows * vocab, st, [&] { return hvdx::launch_distill_grad(g, dtype, st); }),
+                  what);
+}
+
+// What the two directions of the residual connection check alike.
+static int check_norm(int64_t rows, int64_t dim, int dtype, const void* y, const float* post, const void* gate,
+                      int gate_dtype, int64_t gate_rows, float scale, const char* what) {
+  if (int rc = check_rows(rows, dim, HVDX_MAX_NORM_DIM, dtype, "dimension", what)) return rc;
+  if (!isfinite(scale)) return fail(HVDX_ERR_INVALID, "%s: scale is not finite", what);
+  if (!y && (post || gate)) return fail(HVDX_ERR_INVALID, "%s: post and gate need y", what);
+  if (gate && gate_dtype != HVDX_FLOAT32 && gate_dtype != dtype)
+    return fail(HVDX_ERR_INVALID, "%s: gate_dtype %d is neither binary32 nor the rows' type", what, gate_dtype);
+  if (gate && rows > 0 && (gate_rows < 1 || rows % gate_rows))
+    return fail(HVDX_ERR_INVALID, "%s: gate_rows %lld does not divide %lld rows", what, (long long)gate_rows, (long long)rows);
+  return HVDX_OK;
+}
+
+int hvdx_residual_norm(const void* x, int64_t x_stride, const void* y, int64_t y_stride, int dtype, int64_t rows, int64_t dim,
+                       const float* post, const void* gate, int gate_dtype, int64_t gate_rows, float scale,
+                       const float* weight, float eps, void* x_out, void* h_out, float* stats, void* stream) {
+  static const char* what = "hvdx_residual_norm";
+  if (int rc = check_norm(rows, dim, dtype, y, post, gate, gate_dtype, gate_rows, scale, what)) return rc;
+  if (int rc = check_stride("x", x_stride, dim, rows, what)) return rc;
+  if (y)
+    if (int rc = check_stride("y", y_stride, dim, rows, what)) return rc;
+  if (!(eps >= 0.f) || !isfinite(eps)) return fail(HVDX_ERR_INVALID, "%s: eps %g is negative or not finite", what, eps);
+  if (rows == 0) return HVDX_OK;
+  if (!x) return fail(HVDX_ERR_INVALID, "%s: x is NULL", what);
+  if (!x_out && !h_out && !stats) return fail(HVDX_ERR_INVALID, "%s: no output", what);
+  if (!y && x_out) return fail(HVDX_ERR_INVALID, "%s: x_out without y", what);
+  const int es = row_elem_size(dtype), gs = gate && gate_dtype == HVDX_FLOAT32 ? 4 : es;
+  const Buffer in[] = {matrix("x", x, rows, dim, rows > 1 ? x_stride : dim, es), matrix("y", y, rows, dim, rows > 1 ? y_stride : dim, es),
+                       vec("post", post, dim, 4), vec("gate", gate, gate ? rows / gate_rows * dim : 0, gs),
+                       vec("weight", weight, dim, 4)};
+  const Buffer out[] = {matrix("x_out", x_out, rows, dim, dim, es), matrix("h_out", h_out, rows, dim, dim, es),
+                        vec("stats", stats, rows * 2, 4, 8)};
+  const unsigned same[3] = {3, 2, 0};
+  if (int rc = check_buffers(in, 5, out, 3, same, what)) return rc;
+  const hvdx::NormArgs g{x, y, x_stride, y_stride, rows, (int)dim, post, gate, gs == 4, gate ? gate_rows : 1, scale, eps,
+                         weight, x_out, h_out, reinterpret_cast<float2*>(stats)};
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  TimedLaunch phase(HVDX_KERNEL_RESIDUAL_NORM, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * dim, st, -1, true);
+  return launched(timed(HVDX_KERNEL_RESIDUAL_NORM, dtype, rows * dim, st, [&] { return hvdx::launch_norm(g, dtype, st); }), what);
+}
+
+size_t hvdx_residual_norm_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t gate_rows) {
+  if (rows < 1 || rows > kMostRows || dim < 1 || dim > HVDX_MAX_NORM_DIM || gate_rows < 0 || (gate_rows && rows % gate_rows))
+    return 0;
+  const hvdx::NormPlan p = hvdx::norm_plan(rows, gate_rows);
+  return (size_t)((gate_rows && p.segments > 1 ? 3 : 2) * p.blocks * dim * 4);
+}
+
+int hvdx_residual_norm_grad(const void* x, int64_t x_stride, const void* y, int64_t y_stride, const void* dx,
+                            int64_t dx_stride, const void* dh, int64_t dh_stride, int dtype, int64_t rows, int64_t dim,
+                            const float* post, const void* gate, int gate_dtype, int64_t gate_rows, float scale,
+                            const float* weight, const float* stats, void* grad_x, void* grad_y, float* grad_weight,
+                            float* grad_post, void* grad_gate, void* workspace, size_t workspace_bytes, void* stream) {
+  static const char* what = "hvdx_residual_norm_grad";
+  if (int rc = check_norm(rows, dim, dtype, y, post, gate, gate_dtype, gate_rows, scale, what)) return rc;
+  const struct { const char* name; const void* p; int64_t stride; } rowed[] = {
+      {"x", x, x_stride}, {"y", y, y_stride}, {"dx", dx, dx_stride}, {"dh", dh, dh_stride}};
+  for (const auto& m : rowed)
+    if (m.p)
+      if (int rc = check_stride(m.name, m.stride, dim, rows, what)) return rc;
+  if ((grad_y && !y) || (grad_post && !post) || (grad_gate && !gate))
+    return fail(HVDX_ERR_INVALID, "%s: a gradient is asked for without what it belongs to", what);
+  if (rows == 0) return HVDX_OK;
+  if (!x || !stats || (!dx && !dh)) return fail(HVDX_ERR_INVALID, "%s: x, stats, or both dx and dh are NULL", what);
+  if (!grad_x && !grad_y && !grad_weight && !grad_post && !grad_gate) return fail(HVDX_ERR_INVALID, "%s: no output", what);
+  const size_t need = hvdx_residual_norm_grad_workspace_bytes(rows, dim, gate ? gate_rows : 0);
+  if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
+  const int es = row_elem_size(dtype), gs = gate && gate_dtype == HVDX_FLOAT32 ? 4 : es;
+  const int64_t gates = gate ? rows / gate_rows * dim : 0;
+  const auto rows_of = [&](const char* name, const void* p, int64_t stride) {
+    return matrix(name, p, rows, dim, rows > 1 ? stride : dim, es);
+  };
+  const Buffer in[] = {rows_of("x", x, x_stride), rows_of("y", y, y_stride), rows_of("dx", dx, dx_stride),
+                       rows_of("dh", dh, dh_stride), vec("post", post, dim, 4), vec("gate", gate, gates, gs),
+                       vec("weight", weight, dim, 4), vec("stats", stats, rows * 2, 4, 8)};
+  const Buffer out[] = {rows_of("grad_x", grad_x, dim), rows_of("grad_y", grad_y, dim), vec("grad_weight", grad_weight, dim, 4),
+                        vec("grad_post", grad_post, dim, 4), vec("grad_gate", grad_gate, gates, gs),
+                        vec("workspace", workspace, (int64_t)need, 1)};
+  const unsigned same[6] = {1u << 2 | 1u << 3, 1u << 1 | 1u << 2 | 1u << 3, 0, 0, 0, 0};
+  if (int rc = check_buffers(in, 8, out, 6, same, what)) return rc;
+  const hvdx::NormGradArgs g{x, y, dx, dh, x_stride, y_stride, dx_stride, dh_stride, rows, (int)dim, post, gate, gs == 4,
+                             gate ? gate_rows : 1, scale, weight, reinterpret_cast<const float2*>(stats), grad_x, grad_y,
+                             grad_weight, grad_post, grad_gate, static_cast<float*>(workspace),
+                             hvdx::norm_plan(rows, gate ? gate_rows : 0)};
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool sums = grad_weight || grad_post || (grad_gate && g.plan.segments > 1);
+  const int kind = HVDX_KERNEL_RESIDUAL_NORM_GRAD;
+  TimedLaunch phase(kind, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * dim, st, -1, true, sums ? 2 : 1);
+  hipError_t e = timed(kind, dtype, rows * dim, st, [&] { return hvdx::launch_norm_grad(g, dtype, st); });
+  if (e == hipSuccess && sums) e = timed(kind, dtype, rows * dim, st, [&] { return hvdx::launch_norm_grad_sums(g, dtype, st); });
+  return launched(e, what);
+}
+
+}  // extern "C"

@@ -1,0 +1,94 @@
+// Device helpers of the language-model operators (vocab_kernels.hip, norm_kernels.hip): a row's
+// elements as binary32 values whatever its type, and sums over a wavefront or a block.
+#pragma once
+
+#include "internal.hpp"
+
+namespace hvdx {
+namespace {
+
+// Sixteen bytes of a row: `aligned` at a multiple of 16, `loose` at any element.
+template <typename T>
+struct RowTypes;
+template <>
+struct RowTypes<float> {
+  static constexpr int n = 4;
+  typedef float aligned __attribute__((ext_vector_type(4)));
+  typedef float loose __attribute__((ext_vector_type(4), aligned(4)));
+  typedef float wide __attribute__((ext_vector_type(4)));
+};
+template <>
+struct RowTypes<_Float16> {
+  static constexpr int n = 8;
+  typedef _Float16 aligned __attribute__((ext_vector_type(8)));
+  typedef _Float16 loose __attribute__((ext_vector_type(8), aligned(2)));
+  typedef float wide __attribute__((ext_vector_type(8)));
+};
+template <>
+struct RowTypes<__bf16> {
+  static constexpr int n = 8;
+  typedef __bf16 aligned __attribute__((ext_vector_type(8)));
+  typedef __bf16 loose __attribute__((ext_vector_type(8), aligned(2)));
+  typedef float wide __attribute__((ext_vector_type(8)));
+};
+
+template <typename T>
+using Packed = typename RowTypes<T>::aligned;
+template <typename T>
+using Wide = typename RowTypes<T>::wide;
+
+template <typename T>
+__device__ __forceinline__ Packed<T> load_packed(const T* p) {  // any element alignment
+  return *reinterpret_cast<const typename RowTypes<T>::loose*>(p);
+}
+template <typename T>
+__device__ __forceinline__ void store_packed(T* p, Packed<T> v) {
+  *reinterpret_cast<typename RowTypes<T>::loose*>(p) = v;
+}
+template <typename T>
+__device__ __forceinline__ Wide<T> widen(Packed<T> v) {
+  return __builtin_convertvector(v, Wide<T>);
+}
+// Rounded to nearest even, once: what a result in 32 bits becomes in the rows' type.
+template <typename T>
+__device__ __forceinline__ Packed<T> narrow(Wide<T> v) {
+  return __builtin_convertvector(v, Packed<T>);
+}
+
+// 2^x as the hardware gives it: one unit in the last place, and 0 below 2^-126, where a
+// term no longer counts next to the largest one's 1.
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <typename F>
+__device__ __forceinline__ float wave_reduce(float x, F f) {
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) x = f(x, __shfl_xor(x, k));
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  return wave_reduce(x, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return wave_reduce(x, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// A block for each row; grids are two-dimensional, as a dimension has fewer than 2^32 threads.
+constexpr int64_t kGridRow = 1 << 21;
+__device__ __forceinline__ int64_t block_row() { return (int64_t)blockIdx.y * kGridRow + blockIdx.x; }
+inline dim3 row_grid(int64_t blocks) {
+  const int64_t x = blocks < kGridRow ? blocks : kGridRow;
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+
+template <typename F>
+void by_type(int dtype, F f) {
+  if (dtype == HVDX_FLOAT32) f(float{});
+  else if (dtype == HVDX_FLOAT16) f(_Float16{});
+  else f(__bf16{});
+}
+
+}  // namespace
+}  // namespace hvdx

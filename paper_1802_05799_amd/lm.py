@@ -1,0 +1,267 @@
+"""Language-model operators on rows of token positions: what a data-parallel worker computes around
+the matrix products whose gradients `FusedAllreduce` averages.
+
+    teacher = hv.TokenLogprobs(rows, vocab, top=32)       # outputs and workspace, once
+    teacher(teacher_logits, tokens)                       # teacher.top_ids, teacher.top_logprobs, ...
+    loss = hv.DistillLoss(rows, vocab, alternatives=32)
+    loss(logits, teacher.top_ids, teacher.top_logprobs, grad_loss=g, out=grad_logits)  # loss.loss too
+    norm = hv.ResidualNorm(rows, dim, torch.bfloat16, gate_rows=rows, grad=True)
+    norm(x, y, weight, post_weight, gate)                 # norm.x, norm.h
+    norm.grad(y, grad_x, grad_h, weight, post_weight, gate)  # norm.grad_x, norm.grad_y, norm.grad_weight, ...
+
+Each object owns its outputs (fixed tensors, overwritten by its next call) and its workspace, and may
+take fewer rows than it was built for: the outputs' first rows are then the call's.  Calls are
+asynchronous on `stream` (default: torch's current stream of the device); the inputs must be ready
+on that stream and stay until the work is done, as with torch's own calls.  The kernels are
+behind the C-ABI (hvdx_token_logprobs, hvdx_distill, hvdx_residual_norm and their _grad calls, in
+include/hvdx.h, which defines every case: masked logits, absent tokens, rows without any).
+"""
+from __future__ import annotations
+
+import torch
+
+from . import _lib as L
+from .cycle import current_stream
+
+_DTYPE = {torch.float32: L.FLOAT32, torch.float16: L.FLOAT16, torch.bfloat16: L.BFLOAT16}
+
+
+def _rows(name, x, length, most, device):
+    """Checks a matrix of rows; returns (rows, row stride)."""
+    if x.dim() != 2 or x.shape[1] != length or x.shape[0] > most:
+        raise ValueError(f"{name}: shape {tuple(x.shape)}, expected at most {most} rows of {length}")
+    if x.device != device:
+        raise ValueError(f"{name} is on {x.device}, expected {device}")
+    rows, stride = x.shape[0], x.stride()
+    if stride[1] != 1 and length > 1 or rows > 1 and stride[0] < length:
+        raise ValueError(f"{name}: strides {stride}: a row's elements must lie side by side, and rows apart")
+    return rows, max(stride[0], length)
+
+
+def _like(name, x, shape, dtype, device):
+    """Checks a dense operand of fixed shape and type; returns its address."""
+    if x.shape != shape or x.dtype != dtype or x.device != device or not x.is_contiguous():
+        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)} on {x.device}, expected contiguous {dtype} {tuple(shape)} on {device}")
+    return x.data_ptr()
+
+
+def _type(name, dtype):
+    if dtype not in _DTYPE:
+        raise ValueError(f"{name}: type {dtype}, expected float32, float16 or bfloat16")
+    return _DTYPE[dtype]
+
+
+class _Operator:
+    """Device, and the streams that the object's tensors are used on."""
+
+    def _own(self, device, **tensors):
+        self._tensors = [t for t in tensors.values() if t is not None and t.numel()]
+        self._streams = {current_stream(device)}
+        for name, t in tensors.items():
+            setattr(self, name, t)
+
+    def _stream(self, stream):
+        if stream is None:
+            stream = current_stream(self.device)
+        if stream not in self._streams:  # freed memory is then kept until that stream's work is done too
+            other = torch.cuda.ExternalStream(stream, device=self.device)
+            for t in self._tensors:
+                t.record_stream(other)
+            self._streams.add(stream)
+        return stream
+
+
+def _device(device):
+    device = torch.device(device)
+    if device.type != "cuda":
+        raise ValueError(f"the operators run on a GPU, not on {device}")
+    return torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+
+
+class TokenLogprobs(_Operator):
+    """Log probabilities of given tokens under softmax(scale * logits), with each row's entropy and its
+    `top` likeliest tokens: `logprob`, `entropy` [rows] float32, `top_ids` int64 and `top_logprobs`
+    float32 [rows, top] (descending, ties to the lowest index)."""
+
+    def __init__(self, rows: int, vocab: int, top: int = 0, device="cuda"):
+        if rows < 0 or vocab < 1:
+            raise ValueError(f"{rows} rows of {vocab} logits")
+        if not 0 <= top <= min(vocab, L.MAX_TOP):
+            raise ValueError(f"top {top} outside 0..{min(vocab, L.MAX_TOP)}")
+        self.rows, self.vocab, self.top, self.device = rows, vocab, top, _device(device)
+        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=self.device)  # noqa: E731
+        self._bytes = L.hvdx_token_logprobs_workspace_bytes(rows, vocab, top)
+        self._own(self.device, logprob=new(rows), entropy=new(rows), top_ids=new(rows, top, dtype=torch.int64),
+                  top_logprobs=new(rows, top), stats=new(rows, 4), workspace=new(self._bytes, dtype=torch.uint8))
+        self._out = (self.logprob.data_ptr(), self.entropy.data_ptr(), top, self.top_ids.data_ptr(),
+                     self.top_logprobs.data_ptr(), self.stats.data_ptr(), self.workspace.data_ptr(), self._bytes)
+        self.scale = None  # the last call's
+
+    def __call__(self, logits, tokens=None, scale: float = 1.0, stream: int | None = None) -> None:
+        """tokens: int64 [rows], negative for none (log probability 0); without them `logprob` is left as it was."""
+        dtype = _type("logits", logits.dtype)
+        rows, stride = _rows("logits", logits, self.vocab, self.rows, self.device)
+        at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self.device)
+        out = self._out if at else (0, *self._out[1:])
+        L.hvdx_token_logprobs(logits.data_ptr(), stride, dtype, rows, self.vocab, scale, at, *out, self._stream(stream))
+        self.scale = scale
+
+    def grad(self, logits, tokens, grad_logprob, grad_entropy=None, out=None, stream: int | None = None):
+        """The logits' gradient for the last call's `logprob` and `entropy` (grad_logprob, grad_entropy: float32
+        [rows], None for none) into `out` (of the logits' type; may be `logits`; None: a new tensor), which is returned."""
+        if self.scale is None:
+            raise ValueError("grad before the first call")
+        dtype = _type("logits", logits.dtype)
+        rows, stride = _rows("logits", logits, self.vocab, self.rows, self.device)
+        at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self.device)
+        a = 0 if grad_logprob is None else _like("grad_logprob", grad_logprob, (rows,), torch.float32, self.device)
+        b = 0 if grad_entropy is None else _like("grad_entropy", grad_entropy, (rows,), torch.float32, self.device)
+        out, out_stride = _grad_of(logits, out)
+        L.hvdx_token_logprobs_grad(logits.data_ptr(), stride, dtype, rows, self.vocab, self.scale, at,
+                                   self.stats.data_ptr(), a, b, out.data_ptr(), out_stride, self._stream(stream))
+        return out
+
+
+def _grad_of(logits, out):
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif out.dtype != logits.dtype or out.shape != logits.shape:
+        raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, expected {logits.dtype} {tuple(logits.shape)}")
+    return out, _rows("out", out, logits.shape[1], logits.shape[0], logits.device)[1]
+
+
+class DistillLoss(_Operator):
+    """A student's loss against a teacher's alternatives (their tokens and log probabilities, as
+    TokenLogprobs gives them): the Kullback-Leibler divergence of softmax(scale * logits) from them.
+    With `rest`, what the alternatives leave of the teacher's probability is one more outcome, against
+    the student's probability of every token not listed; without, the alternatives' probabilities
+    are taken to be all (any scores then do).  `loss`: float32 [rows]."""
+
+    def __init__(self, rows: int, vocab: int, alternatives: int, rest: bool = True, device="cuda"):
+        if rows < 0 or vocab < 1:
+            raise ValueError(f"{rows} rows of {vocab} logits")
+        if not 1 <= alternatives <= L.MAX_TOP:
+            raise ValueError(f"{alternatives} alternatives outside 1..{L.MAX_TOP}")
+        self.rows, self.vocab, self.alternatives, self.rest = rows, vocab, alternatives, bool(rest)
+        self.device = _device(device)
+        self._bytes = L.hvdx_distill_workspace_bytes(rows, vocab)
+        self._own(self.device, loss=torch.empty(rows, device=self.device), stats=torch.empty(rows, 4, device=self.device),
+                  workspace=torch.empty(self._bytes, dtype=torch.uint8, device=self.device))
+        self.scale = None  # the last call's
+
+    def _inputs(self, logits, ids, logprobs):
+        dtype = _type("logits", logits.dtype)
+        rows, stride = _rows("logits", logits, self.vocab, self.rows, self.device)
+        shape = (rows, self.alternatives)
+        return rows, (logits.data_ptr(), stride, dtype, rows, self.vocab), (
+            _like("ids", ids, shape, torch.int64, self.device), _like("logprobs", logprobs, shape, torch.float32, self.device),
+            self.alternatives, self.rest)
+
+    def __call__(self, logits, ids, logprobs, scale: float = 1.0, grad_loss=None, out=None, stream: int | None = None) -> None:
+        """ids: int64 [rows, alternatives], negative for none; logprobs: float32.  With `grad_loss` (float32 [rows]) and
+        `out` (of the logits' type; may be `logits`) the logits' gradient is written too, in the same pass."""
+        rows, head, teacher = self._inputs(logits, ids, logprobs)
+        if (grad_loss is None) != (out is None):
+            raise ValueError("grad_loss and out go together")
+        g = at = out_stride = 0
+        if out is not None:
+            g = _like("grad_loss", grad_loss, (rows,), torch.float32, self.device)
+            at, out_stride = out.data_ptr(), _grad_of(logits, out)[1]
+        L.hvdx_distill(*head, scale, *teacher, g, self.loss.data_ptr(), self.stats.data_ptr(), at, out_stride,
+                       self.workspace.data_ptr(), self._bytes, self._stream(stream))
+        self.scale = scale
+
+    def grad(self, logits, ids, logprobs, grad_loss, out=None, stream: int | None = None):
+        """The logits' gradient for the last call's `loss`, into `out` (may be `logits`; None: a new tensor)."""
+        if self.scale is None:
+            raise ValueError("grad before the first call")
+        rows, head, teacher = self._inputs(logits, ids, logprobs)
+        g = _like("grad_loss", grad_loss, (rows,), torch.float32, self.device)
+        out, out_stride = _grad_of(logits, out)
+        L.hvdx_distill_grad(*head, self.scale, *teacher, self.stats.data_ptr(), g, out.data_ptr(), out_stride,
+                            self._stream(stream))
+        return out
+
+
+class ResidualNorm(_Operator):
+    """The residual connection from one block to the next: x' = x + scale * gate * norm(y) * post_weight and
+    h = norm(x') * weight, norm(v) = v / sqrt(mean v^2 + eps) over a row of `dim`.  `x` (x') and `h` hold the last
+    call's results, `stats` what `grad` takes of them.
+
+    `post`: y is normed before it is added.  `gate_rows`: 0 for no gate, else how many rows in a run share a
+    vector of it (`rows`: one vector, a parameter; 1: a vector for each row), of `gate_dtype` (float32 or
+    the rows' type).  `block=False`: no y, just the norm of x (`x` is then the call's own x).  `grad`: make the gradients' tensors
+    (grad_x, grad_y of the rows' type; grad_weight, grad_post float32 [dim]; grad_gate of the gate's type) too."""
+
+    def __init__(self, rows: int, dim: int, dtype, post: bool = True, gate_rows: int = 0, gate_dtype=None, eps: float = 1e-6,
+                 block: bool = True, grad: bool = False, device="cuda"):
+        if rows < 1 or not 1 <= dim <= L.MAX_NORM_DIM:
+            raise ValueError(f"{rows} rows of {dim}, expected rows of 1..{L.MAX_NORM_DIM}")
+        if gate_rows < 0 or gate_rows and rows % gate_rows:
+            raise ValueError(f"gate_rows {gate_rows} does not divide {rows} rows")
+        post, gate_rows = post and block, gate_rows if block else 0
+        self.rows, self.dim, self.dtype, self.post, self.gate_rows = rows, dim, dtype, post, gate_rows
+        self.block, self.eps, self.device = block, eps, _device(device)
+        self._type = _type("rows", dtype)
+        self.gate_dtype = gate_dtype or torch.float32
+        if gate_rows and self.gate_dtype not in (torch.float32, dtype):
+            raise ValueError(f"gate_dtype {gate_dtype}, expected float32 or {dtype}")
+        self._gate = (rows // gate_rows, dim) if gate_rows else None
+        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=self.device)  # noqa: E731
+        own = dict(h=new(rows, dim, dtype=dtype), stats=new(rows, 2))
+        own["x"] = new(rows, dim, dtype=dtype) if block else None
+        self._bytes = 0
+        if grad:
+            self._bytes = L.hvdx_residual_norm_grad_workspace_bytes(rows, dim, gate_rows)
+            own.update(grad_x=new(rows, dim, dtype=dtype), grad_y=new(rows, dim, dtype=dtype) if block else None,
+                       grad_weight=new(dim), grad_post=new(dim) if post else None,
+                       grad_gate=new(*self._gate, dtype=self.gate_dtype) if gate_rows else None,
+                       workspace=new(self._bytes, dtype=torch.uint8))
+        self._with_grad = grad
+        self._own(self.device, **own)
+
+    def _row_input(self, name, x):
+        if x.dtype != self.dtype:
+            raise ValueError(f"{name}: type {x.dtype}, expected {self.dtype}")
+        rows, stride = _rows(name, x, self.dim, self.rows, self.device)
+        if rows != self.rows:
+            raise ValueError(f"{name}: {rows} rows, expected {self.rows}")
+        return x.data_ptr(), stride
+
+    def _parameters(self, weight, post, gate):
+        if (post is not None) != self.post or (gate is not None) != bool(self.gate_rows):
+            raise ValueError("post_weight and gate must be given exactly if the object was built with them")
+        f32, shape, d = torch.float32, (self.dim,), self.device
+        return (0 if weight is None else _like("weight", weight, shape, f32, d), 0 if post is None else _like("post_weight", post, shape, f32, d),
+                0 if gate is None else _like("gate", gate if gate.dim() == 2 else gate.view(1, -1), self._gate, self.gate_dtype, d))
+
+    def __call__(self, x, y, weight, post_weight=None, gate=None, scale: float = 1.0, stream: int | None = None) -> None:
+        """x, y: [rows, dim]; weight, post_weight: float32 [dim] (weight None: 1); gate: [rows / gate_rows, dim]."""
+        w, p, q = self._parameters(weight, post_weight, gate)
+        if (y is not None) != self.block:
+            raise ValueError("y must be given exactly if the object was built with block=True")
+        ys = self._row_input("y", y) if y is not None else (0, 0)
+        L.hvdx_residual_norm(*self._row_input("x", x), *ys, self._type, self.rows, self.dim, p, q, _DTYPE[self.gate_dtype],
+                             self.gate_rows, scale, w, self.eps, self.x.data_ptr() if self.block else 0, self.h.data_ptr(),
+                             self.stats.data_ptr(), self._stream(stream))
+        if not self.block:
+            self.x = x
+
+    def grad(self, y, grad_x, grad_h, weight, post_weight=None, gate=None, scale: float = 1.0, stream: int | None = None) -> None:
+        """From the last call's `x` and `stats` and the gradients of its `x` and `h` (None for none of one of them): sets
+        `grad_x`, `grad_y`, `grad_weight`, `grad_post`, `grad_gate`."""
+        if not self._with_grad:
+            raise ValueError("built without grad=True")
+        if self.x is None:
+            raise ValueError("grad before the first call")
+        w, p, q = self._parameters(weight, post_weight, gate)
+        if (y is not None) != self.block:
+            raise ValueError("y must be given exactly if the object was built with block=True")
+        none = (0, 0)
+        ys, ds = (self._row_input("y", y) if y is not None else none), (self._row_input("grad_x", grad_x) if grad_x is not None else none)
+        hs = self._row_input("grad_h", grad_h) if grad_h is not None else none
+        at = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
+        L.hvdx_residual_norm_grad(*self._row_input("x", self.x), *ys, *ds, *hs, self._type, self.rows, self.dim, p, q,
+                                  _DTYPE[self.gate_dtype], self.gate_rows, scale, w, self.stats.data_ptr(), at(self.grad_x),
+                                  at(self.grad_y), at(self.grad_weight), at(self.grad_post),
+                                  at(self.grad_gate), self.workspace.data_ptr(), self._bytes, self._stream(stream))

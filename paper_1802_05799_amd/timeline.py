@@ -40,6 +40,12 @@ KIND_NAMES = {
     L.KERNEL_AG_UNPACK: "allgather + copy out",
     L.KERNEL_RING_SMALL: "whole ring (one launch)",
     L.KERNEL_CYCLE_SMALL: "copy in + whole ring + copy out (one launch)",
+    L.KERNEL_LOGPROBS: "token log probabilities",
+    L.KERNEL_LOGPROBS_GRAD: "token log probabilities' gradient",
+    L.KERNEL_DISTILL: "distillation loss",
+    L.KERNEL_DISTILL_GRAD: "distillation gradient",
+    L.KERNEL_RESIDUAL_NORM: "residual norm",
+    L.KERNEL_RESIDUAL_NORM_GRAD: "residual norm's gradient",
 }
 
 
