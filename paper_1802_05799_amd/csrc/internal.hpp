@@ -259,7 +259,12 @@ struct LogprobArgs {
   int64_t* top_ids;
   float* top_logprobs;
   float4* stats;  // row's maximum, log of its sum, entropy
+  int parts;      // blocks a row (row_parts); with more than one:
+  float4* part_sums;    // [rows][parts]
+  uint64_t* part_keys;  // [rows][parts][top]
 };
+int row_parts(int64_t rows, int64_t vocab);
+hipError_t launch_logprobs_join(const LogprobArgs& g, int dtype, hipStream_t stream);  // after the other, with parts > 1
 hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream);
 struct LogprobGradArgs {
   const void* logits;

@@ -120,8 +120,9 @@ int check_distill(int64_t rows, int64_t vocab, int dtype, int64_t stride, float 
 extern "C" {
 
 size_t hvdx_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int top) {
-  (void)rows, (void)vocab, (void)top;
-  return 0;
+  if (rows < 1 || rows > kMostRows || vocab < 1 || vocab > HVDX_MAX_VOCAB || top < 0 || top > HVDX_MAX_TOP) return 0;
+  const int parts = hvdx::row_parts(rows, vocab);
+  return parts == 1 ? 0 : (size_t)rows * parts * (16 + 8 * top);
 }
 
 int hvdx_token_logprobs(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
@@ -145,11 +146,16 @@ int hvdx_token_logprobs(const void* logits, int64_t stride, int dtype, int64_t r
                         vec("workspace", workspace, (int64_t)need, 1)};
   const unsigned same[6] = {};
   if (int rc = check_buffers(in, 2, out, 6, same, what)) return rc;
+  const int parts = hvdx::row_parts(rows, vocab);
+  float4* const sums = static_cast<float4*>(workspace);
   const hvdx::LogprobArgs g{logits, stride, rows, (int)vocab, scale, tokens, logprob, entropy, top, top_ids, top_logprobs,
-                            reinterpret_cast<float4*>(stats)};
+                            reinterpret_cast<float4*>(stats), parts, sums, reinterpret_cast<uint64_t*>(sums + rows * parts)};
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  TimedLaunch phase(HVDX_KERNEL_LOGPROBS, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
-  return launched(timed(HVDX_KERNEL_LOGPROBS, dtype, rows * vocab, st, [&] { return hvdx::launch_logprobs(g, dtype, st); }), what);
+  const int kind = HVDX_KERNEL_LOGPROBS;
+  TimedLaunch phase(kind, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true, parts > 1 ? 2 : 1);
+  hipError_t e = timed(kind, dtype, rows * vocab, st, [&] { return hvdx::launch_logprobs(g, dtype, st); });
+  if (e == hipSuccess && parts > 1) e = timed(kind, dtype, rows * vocab, st, [&] { return hvdx::launch_logprobs_join(g, dtype, st); });
+  return launched(e, what);
 }
 
 int hvdx_token_logprobs_grad(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,

@@ -13,6 +13,11 @@
 namespace hvdx {
 namespace {
 
+// Rows are split over blocks where there are too few of them to fill the chip: into parts of at least
+// kPartLeast elements, until there are kBlocksWanted blocks.
+constexpr int64_t kBlocksWanted = 1024, kPartLeast = 4096;
+constexpr int kPartsMost = 64;  // one lane each when they are joined
+
 constexpr float kNone = -3.402823466e38f;  // the maximum of nothing: finite, so that -inf minus it is no NaN
 constexpr float kFar = -1000.f;            // 2^kFar is 0; a clamp for what 0 is multiplied by
 
@@ -89,83 +94,253 @@ __device__ __forceinline__ int key_position(uint64_t k) { return (int)~(uint32_t
 
 constexpr int kWaves = 4;
 
+// The `k` first of a block's keys.  Each thread has the first of its own as `best`, at a coarser grain
+// (the position of its vector); the block's 64 groups of W threads have one first key each, and the
+// k-th of those is a bound that at least k keys reach: what lies below it cannot be among the k
+// first.  Little reaches it (k = 32 of 131,072 normal values: about 45), so the threads with any
+// collect those into LDS, where each finds its rank by counting.  Where more reach it than LDS
+// holds, k rounds over all keys find them one by one.
+constexpr int kCandidates = 1024;
+template <int W>
+struct TopLds {
+  uint64_t group[64], candidate[kCandidates], best[W], bound;
+  int count;
+};
+template <int W, typename Collect, typename Below, typename Emit>
+__device__ void select_top(int k, uint64_t best, TopLds<W>& lds, Collect collect, Below below, Emit emit) {
+  constexpr int NT = 64 * W;
+  const int tid = threadIdx.x;
+  uint64_t first = best;
+#pragma unroll
+  for (int j = 1; j < W; j *= 2) {
+    const uint64_t other = __shfl_xor((unsigned long long)first, j);
+    if (other > first) first = other;
+  }
+  if (tid % W == 0) lds.group[tid / W] = first;
+  if (tid == 0) lds.count = 0;
+  __syncthreads();
+  if (tid < 64) {
+    const uint64_t mine = lds.group[tid];
+    int rank = 0;
+#pragma unroll 16
+    for (int j = 0; j < 64; ++j) {
+      const uint64_t other = lds.group[j];
+      rank += other > mine || (other == mine && j < tid);
+    }
+    if (rank == k - 1) lds.bound = mine;
+  }
+  __syncthreads();
+  const uint64_t bound = lds.bound;
+  if (best && best >= bound)
+    collect(bound, [&](uint64_t key) {
+      const int at = atomicAdd(&lds.count, 1);
+      if (at < kCandidates) lds.candidate[at] = key;
+    });
+  __syncthreads();
+  const int count = lds.count;
+  if (count <= kCandidates) {
+    for (int i = tid; i < count; i += NT) {
+      const uint64_t mine = lds.candidate[i];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < count; ++j) rank += lds.candidate[j] > mine;
+      if (rank < k) emit(rank, mine);
+    }
+    for (int i = count + tid; i < k; i += NT) emit(i, 0);  // there are no more
+    return;
+  }
+  uint64_t last = ~0ull;
+  for (int r = 0; r < k; ++r) {
+    uint64_t next = below(last);
+#pragma unroll
+    for (int j = 1; j < 64; j *= 2) {
+      const uint64_t other = __shfl_xor((unsigned long long)next, j);
+      if (other > next) next = other;
+    }
+    __syncthreads();
+    if (tid % 64 == 0) lds.best[tid / 64] = next;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+      if (lds.best[w] > next) next = lds.best[w];
+    if (tid == 0) emit(r, next);
+    last = next;
+  }
+}
+
+// What a row's sums give, and one of its alternatives.
+__device__ __forceinline__ void finish_logprobs(const LogprobArgs& g, int64_t row, float z_token, int64_t token, Online o) {
+  const bool none = o.s == 0.f;
+  const float lse = logf(o.s), entropy = none ? 0.f : lse - kLn2 * o.a / o.s;
+  if (g.logprob) {
+    float lp = 0.f;
+    if (token >= g.vocab) lp = __builtin_nanf("");
+    else if (token >= 0) lp = none ? -__builtin_inff() : (z_token - o.m) * g.scale - lse;
+    g.logprob[row] = lp;
+  }
+  if (g.entropy) g.entropy[row] = entropy;
+  if (g.stats) g.stats[row] = make_float4(o.m, lse, entropy, 0.f);
+}
+__device__ __forceinline__ void emit_top(const LogprobArgs& g, int64_t row, int rank, uint64_t key, Online o) {
+  const bool broken = !(o.s == o.s);
+  g.top_ids[row * g.top + rank] = broken ? -1 : key_position(key);
+  g.top_logprobs[row * g.top + rank] = broken ? __builtin_nanf("")
+                                       : o.s == 0.f ? -__builtin_inff()
+                                                    : (key_value(key) - o.m) * g.scale - logf(o.s);
+}
+
+// A block has one of a row's `parts`: all of it, and the results, or a stretch of its vectors, whose sums and
+// first keys go to the workspace for logprobs_join_kernel.  kBatch vectors are loaded at once, and
+// the sums rescaled once for each batch.
+constexpr int kBatch = 4;
+template <typename T, int W>
+__global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
+  constexpr int NT = 64 * W, N = RowTypes<T>::n;
+  __shared__ float parts[W][3];
+  __shared__ TopLds<W> top;
+  const int64_t block = block_row();
+  if (block >= g.rows * g.parts) return;
+  const int64_t row = g.parts == 1 ? block : block / g.parts;
+  const int part = g.parts == 1 ? 0 : (int)(block % g.parts);
+  const T* z = static_cast<const T*>(g.logits) + row * g.stride;
+  const float c = g.scale * kLog2e;
+  const Cut<T> cut(z, g.vocab);
+  const int v0 = (int)((int64_t)cut.nvec * part / g.parts), v1 = (int)((int64_t)cut.nvec * (part + 1) / g.parts);
+  const int edges = part == 0 ? cut.edges : 0;
+  const int64_t token = g.logprob ? g.tokens[row] : -1;
+  const float z_token = token >= 0 && token < g.vocab ? (float)z[token] : 0.f;
+  Online o;
+  float high = -__builtin_inff();  // the thread's largest, and where its vector (or edge element) starts
+  int high_at = v0 + (int)threadIdx.x < v1 ? cut.start(v0 + threadIdx.x) : (int)threadIdx.x < edges ? cut.edge(threadIdx.x) : -1;
+  for (int i = v0 + threadIdx.x; i < v1; i += kBatch * NT) {
+    Packed<T> p[kBatch];
+    bool there[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      there[u] = i + u * NT < v1;
+      if (there[u]) p[u] = load_packed(z + cut.start(i + u * NT));
+    }
+    Wide<T> x[kBatch];
+    float hi = kNone;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      x[u] = there[u] ? widen<T>(p[u]) : Wide<T>(-__builtin_inff());
+      float h = x[u][0];
+#pragma unroll
+      for (int k = 1; k < N; ++k) h = fmaxf(h, x[u][k]);
+      if (h > high) {
+        high = h;
+        high_at = cut.start(i + u * NT);
+      }
+      hi = fmaxf(hi, h);
+    }
+    if (hi > o.m) o.rise(hi, c);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+#pragma unroll
+      for (int k = 0; k < N; ++k) o.add(x[u][k], c);
+  }
+  if ((int)threadIdx.x < edges) {
+    const float x = (float)z[cut.edge(threadIdx.x)];
+    if (high_at < 0 || key_of(x, cut.edge(threadIdx.x)) > key_of(high, high_at)) {  // it may stand before the vectors
+      high = x;
+      high_at = cut.edge(threadIdx.x);
+    }
+    if (x > o.m) o.rise(x, c);
+    o.add(x, c);
+  }
+  o = block_join<W>(o, c, parts);
+  const bool whole = g.parts == 1;
+  if (threadIdx.x == 0) {
+    if (whole) finish_logprobs(g, row, z_token, token, o);
+    else g.part_sums[block] = make_float4(o.m, o.s, o.a, 0.f);
+  }
+  if (!g.top) return;
+  select_top<W>(
+      g.top, high_at < 0 ? 0 : key_of(high, high_at), top,
+      [&](uint64_t bound, auto push) {
+        for (int i = v0 + threadIdx.x; i < v1; i += kBatch * NT) {
+          Packed<T> p[kBatch];
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u)
+            if (i + u * NT < v1) p[u] = load_packed(z + cut.start(i + u * NT));
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u) {
+            if (i + u * NT >= v1) break;
+            const int start = cut.start(i + u * NT);
+            const Wide<T> x = widen<T>(p[u]);
+            float h = x[0];
+#pragma unroll
+            for (int k = 1; k < N; ++k) h = fmaxf(h, x[k]);
+            if (key_of(h, start) < bound) continue;
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+              if (key_of(x[k], start) >= bound) push(key_of(x[k], start + k));
+          }
+        }
+        if ((int)threadIdx.x < edges) {
+          const uint64_t key = key_of((float)z[cut.edge(threadIdx.x)], cut.edge(threadIdx.x));
+          if (key >= bound) push(key);
+        }
+      },
+      [&](uint64_t last) {
+        uint64_t next = 0;
+        auto take = [&](float x, int at) {
+          const uint64_t key = key_of(x, at);
+          if (key < last && key > next) next = key;
+        };
+        for (int i = v0 + threadIdx.x; i < v1; i += NT) {
+          const Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
+#pragma unroll
+          for (int k = 0; k < N; ++k) take(x[k], cut.start(i) + k);
+        }
+        if ((int)threadIdx.x < edges) take((float)z[cut.edge(threadIdx.x)], cut.edge(threadIdx.x));
+        return next;
+      },
+      [&](int rank, uint64_t key) {
+        if (whole) emit_top(g, row, rank, key, o);
+        else g.part_keys[block * g.top + rank] = key;
+      });
+}
+
+// A row's results from its parts'.
 template <typename T>
-__global__ __launch_bounds__(64 * kWaves) void logprobs_kernel(LogprobArgs g) {
-  constexpr int NT = 64 * kWaves, N = RowTypes<T>::n;
+__global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs g) {
+  constexpr int NT = 64 * kWaves;
   __shared__ float parts[kWaves][3];
-  __shared__ uint64_t keys[kWaves];
+  __shared__ TopLds<kWaves> top;
   const int64_t row = block_row();
   if (row >= g.rows) return;
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   const float c = g.scale * kLog2e;
-  const Cut<T> cut(z, g.vocab);
+  const int64_t token = g.logprob ? g.tokens[row] : -1;
+  const float z_token = token >= 0 && token < g.vocab ? (float)z[token] : 0.f;
+  const uint64_t* keys = g.part_keys + row * g.parts * g.top;
+  const int nkeys = g.parts * g.top;
   Online o;
-  for (int i = threadIdx.x; i < cut.nvec; i += NT) {
-    const Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
-    float hi = x[0];
-#pragma unroll
-    for (int k = 1; k < N; ++k) hi = fmaxf(hi, x[k]);
-    if (hi > o.m) o.rise(hi, c);
-#pragma unroll
-    for (int k = 0; k < N; ++k) o.add(x[k], c);
+  if ((int)threadIdx.x < g.parts) {
+    const float4 s = g.part_sums[row * g.parts + threadIdx.x];
+    o = Online{s.x, s.y, s.z};
   }
-  if ((int)threadIdx.x < cut.edges) {
-    const float x = (float)z[cut.edge(threadIdx.x)];
-    if (x > o.m) o.rise(x, c);
-    o.add(x, c);
-  }
+  uint64_t best = 0;
+  for (int i = threadIdx.x; i < nkeys; i += NT)
+    if (keys[i] > best) best = keys[i];
   o = block_join<kWaves>(o, c, parts);
-  const bool none = o.s == 0.f, broken = !(o.s == o.s);
-  const float lse = logf(o.s);
-  if (threadIdx.x == 0) {
-    const float entropy = none ? 0.f : lse - kLn2 * o.a / o.s;
-    if (g.logprob) {
-      const int64_t t = g.tokens[row];
-      float lp = 0.f;
-      if (t >= g.vocab) lp = __builtin_nanf("");
-      else if (t >= 0) lp = none ? -__builtin_inff() : ((float)z[t] - o.m) * g.scale - lse;
-      g.logprob[row] = lp;
-    }
-    if (g.entropy) g.entropy[row] = entropy;
-    if (g.stats) g.stats[row] = make_float4(o.m, lse, entropy, 0.f);
-  }
+  if (threadIdx.x == 0) finish_logprobs(g, row, z_token, token, o);
   if (!g.top) return;
-  if (broken) {
-    for (int k = threadIdx.x; k < g.top; k += NT) {
-      g.top_ids[row * g.top + k] = -1;
-      g.top_logprobs[row * g.top + k] = __builtin_nanf("");
-    }
-    return;
-  }
-  uint64_t below = ~0ull;
-  for (int k = 0; k < g.top; ++k) {
-    uint64_t best = 0;
-    auto take = [&](float x, int at) {
-      const uint64_t key = key_of(x, at);
-      if (key < below && key > best) best = key;
-    };
-    for (int i = threadIdx.x; i < cut.nvec; i += NT) {
-      const Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
-#pragma unroll
-      for (int e = 0; e < N; ++e) take(x[e], cut.start(i) + e);
-    }
-    if ((int)threadIdx.x < cut.edges) take((float)z[cut.edge(threadIdx.x)], cut.edge(threadIdx.x));
-#pragma unroll
-    for (int j = 1; j < 64; j *= 2) {
-      const uint64_t other = __shfl_xor((unsigned long long)best, j);
-      if (other > best) best = other;
-    }
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) keys[threadIdx.x / 64] = best;
-    __syncthreads();
-    for (int w = 0; w < kWaves; ++w)
-      if (keys[w] > best) best = keys[w];
-    if (threadIdx.x == 0) {
-      g.top_ids[row * g.top + k] = key_position(best);
-      g.top_logprobs[row * g.top + k] = none ? -__builtin_inff() : (key_value(best) - o.m) * g.scale - lse;
-    }
-    below = best;
-  }
+  select_top<kWaves>(
+      g.top, best, top,
+      [&](uint64_t bound, auto push) {
+        for (int i = threadIdx.x; i < nkeys; i += NT)
+          if (keys[i] && keys[i] >= bound) push(keys[i]);
+      },
+      [&](uint64_t last) {
+        uint64_t next = 0;
+        for (int i = threadIdx.x; i < nkeys; i += NT)
+          if (keys[i] < last && keys[i] > next) next = keys[i];
+        return next;
+      },
+      [&](int rank, uint64_t key) { emit_top(g, row, rank, key, o); });
 }
 
 // dz_v = s [ a (delta - p_v) - b p_v (log p_v + H) ] = p_v (C0 + C1 d_v) + s a delta, d_v in base 2.
@@ -460,9 +635,26 @@ __global__ __launch_bounds__(64 * kWaves) void distill_grad_kernel(DistillArgs g
 
 }  // namespace
 
+int row_parts(int64_t rows, int64_t vocab) {
+  int64_t parts = (kBlocksWanted + rows - 1) / rows;
+  if (parts > vocab / kPartLeast) parts = vocab / kPartLeast;
+  return parts < 1 ? 1 : parts > kPartsMost ? kPartsMost : (int)parts;
+}
+
 hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream) {
   by_type(dtype, [&](auto t) {
-    HVDX_LAUNCH(logprobs_kernel<decltype(t)>, row_grid(g.rows), dim3(64 * kWaves), 0, stream, g);
+    using T = decltype(t);
+    if (g.vocab / RowTypes<T>::n <= 256)
+      HVDX_LAUNCH((logprobs_kernel<T, 1>), row_grid(g.rows * g.parts), dim3(64), 0, stream, g);
+    else
+      HVDX_LAUNCH((logprobs_kernel<T, kWaves>), row_grid(g.rows * g.parts), dim3(64 * kWaves), 0, stream, g);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_logprobs_join(const LogprobArgs& g, int dtype, hipStream_t stream) {
+  by_type(dtype, [&](auto t) {
+    HVDX_LAUNCH(logprobs_join_kernel<decltype(t)>, row_grid(g.rows), dim3(64 * kWaves), 0, stream, g);
   });
   return hipGetLastError();
 }
