@@ -307,14 +307,18 @@ struct NormArgs {
   const float* weight;
   void *x_out, *h_out;  // rows end to end
   float2* stats;        // the norms' factors: of y (1 without its norm), of x_out
+  int64_t row_step;     // of a block, set by the launch
 };
 hipError_t launch_norm(const NormArgs& g, int dtype, hipStream_t stream);
-// How a backward pass's rows are dealt out: `groups` of `span` rows share a vector of the gate; a block has
-// one of a group's `segments`, of `seg_rows` rows, or (one segment) `per_block` whole groups.
+// How a backward pass's rows are dealt out to units (a block's row slots): `groups` of `span` rows share a
+// vector of the gate; a unit has one of a group's `segments`, or (one segment) whole groups, of
+// unit_rows rows at most.
 struct NormPlan {
-  int64_t groups, span, segments, seg_rows, per_block, blocks;
+  int64_t groups, span, segments, unit_rows, units, blocks;
 };
-NormPlan norm_plan(int64_t rows, int64_t gate_rows);
+NormPlan norm_plan(int64_t rows, int64_t dim, int64_t gate_rows);
+// Rows of partial sums of the gate's gradient: a block's for one group, a unit's for segments of several.
+inline int64_t norm_gate_partials(const NormPlan& p) { return p.groups == 1 ? p.blocks : p.segments > 1 ? p.units : 0; }
 struct NormGradArgs {
   const void *x, *y, *dx, *dh;
   int64_t x_stride, y_stride, dx_stride, dh_stride, rows;
@@ -329,7 +333,7 @@ struct NormGradArgs {
   void *grad_x, *grad_y;
   float *grad_weight, *grad_post;
   void* grad_gate;
-  float* partial;  // blocks x dim for each of weight, post, and gate with more than one segment
+  float* partial;  // [2 blocks + norm_gate_partials][dim]: weight, post, gate
   NormPlan plan;
 };
 hipError_t launch_norm_grad(const NormGradArgs& g, int dtype, hipStream_t stream);

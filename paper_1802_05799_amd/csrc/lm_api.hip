@@ -274,7 +274,7 @@ int hvdx_residual_norm(const void* x, int64_t x_stride, const void* y, int64_t y
   const unsigned same[3] = {3, 2, 0};
   if (int rc = check_buffers(in, 5, out, 3, same, what)) return rc;
   const hvdx::NormArgs g{x, y, x_stride, y_stride, rows, (int)dim, post, gate, gs == 4, gate ? gate_rows : 1, scale, eps,
-                         weight, x_out, h_out, reinterpret_cast<float2*>(stats)};
+                         weight, x_out, h_out, reinterpret_cast<float2*>(stats), 0};
   const hipStream_t st = static_cast<hipStream_t>(stream);
   TimedLaunch phase(HVDX_KERNEL_RESIDUAL_NORM, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * dim, st, -1, true);
   return launched(timed(HVDX_KERNEL_RESIDUAL_NORM, dtype, rows * dim, st, [&] { return hvdx::launch_norm(g, dtype, st); }), what);
@@ -283,8 +283,8 @@ int hvdx_residual_norm(const void* x, int64_t x_stride, const void* y, int64_t y
 size_t hvdx_residual_norm_grad_workspace_bytes(int64_t rows, int64_t dim, int64_t gate_rows) {
   if (rows < 1 || rows > kMostRows || dim < 1 || dim > HVDX_MAX_NORM_DIM || gate_rows < 0 || (gate_rows && rows % gate_rows))
     return 0;
-  const hvdx::NormPlan p = hvdx::norm_plan(rows, gate_rows);
-  return (size_t)((gate_rows && p.segments > 1 ? 3 : 2) * p.blocks * dim * 4);
+  const hvdx::NormPlan p = hvdx::norm_plan(rows, dim, gate_rows);
+  return (size_t)((2 * p.blocks + (gate_rows ? hvdx::norm_gate_partials(p) : 0)) * dim * 4);
 }
 
 int hvdx_residual_norm_grad(const void* x, int64_t x_stride, const void* y, int64_t y_stride, const void* dx,
@@ -322,9 +322,9 @@ int hvdx_residual_norm_grad(const void* x, int64_t x_stride, const void* y, int6
   const hvdx::NormGradArgs g{x, y, dx, dh, x_stride, y_stride, dx_stride, dh_stride, rows, (int)dim, post, gate, gs == 4,
                              gate ? gate_rows : 1, scale, weight, reinterpret_cast<const float2*>(stats), grad_x, grad_y,
                              grad_weight, grad_post, grad_gate, static_cast<float*>(workspace),
-                             hvdx::norm_plan(rows, gate ? gate_rows : 0)};
+                             hvdx::norm_plan(rows, dim, gate ? gate_rows : 0)};
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool sums = grad_weight || grad_post || (grad_gate && g.plan.segments > 1);
+  const bool sums = grad_weight || grad_post || (grad_gate && hvdx::norm_gate_partials(g.plan));
   const int kind = HVDX_KERNEL_RESIDUAL_NORM_GRAD;
   TimedLaunch phase(kind, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * dim, st, -1, true, sums ? 2 : 1);
   hipError_t e = timed(kind, dtype, rows * dim, st, [&] { return hvdx::launch_norm_grad(g, dtype, st); });

@@ -8,7 +8,7 @@
 //   dw_post = sum over rows of du yh,  dy = r_y (du w_post - yh mean(du w_post yh)).
 // Sums, statistics and the weights' gradients are in binary32.  Bound: memory; a row stays in
 // registers between its reads and its writes.  A thread keeps the same columns for every row of its
-// block, so that the sums over rows stay in registers too; blocks write theirs to the
+// block, so that the weights and the sums over rows stay in registers too; blocks write their sums to the
 // workspace, and a second launch adds those in a fixed order.
 #include <type_traits>
 
@@ -17,312 +17,380 @@
 namespace hvdx {
 namespace {
 
-template <typename T>
-__device__ __forceinline__ Wide<T> load_some(const T* p, int count) {  // elements past `count` are 0
-  if (count >= RowTypes<T>::n) return widen<T>(load_packed(p));
-  Wide<T> v = 0.f;
-#pragma unroll
-  for (int k = 0; k < RowTypes<T>::n; ++k)
-    if (k < count) v[k] = (float)p[k];
-  return v;
+// N elements of a row side by side (16 bytes' worth, or one where a row has fewer), as they lie and in binary32.
+template <typename T, int N>
+struct Elems {
+  typedef T raw __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+  typedef T packed __attribute__((ext_vector_type(N)));
+  typedef float wide __attribute__((ext_vector_type(N)));
+};
+template <int N>
+using Floats = typename Elems<float, N>::wide;
+
+template <int N, typename T>
+__device__ __forceinline__ Floats<N> load_elems(const T* p) {
+  const typename Elems<T, N>::packed v = *reinterpret_cast<const typename Elems<T, N>::raw*>(p);
+  return __builtin_convertvector(v, Floats<N>);
 }
-template <typename T>
-__device__ __forceinline__ void store_some(T* p, Wide<T> v, int count) {
-  if (count >= RowTypes<T>::n) {
-    store_packed(p, narrow<T>(v));
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < RowTypes<T>::n; ++k)
-    if (k < count) p[k] = (T)v[k];
+template <int N, typename T>
+__device__ __forceinline__ void store_elems(T* p, Floats<N> v) {
+  *reinterpret_cast<typename Elems<T, N>::raw*>(p) = __builtin_convertvector(v, typename Elems<T, N>::packed);
 }
-// As many binary32 values as the rows' type has in 16 bytes.
-template <typename T>
-__device__ __forceinline__ Wide<T> load_floats(const float* p, int count) {
-  Wide<T> v = 0.f;
-  constexpr int n = RowTypes<T>::n;
-  if (count >= n) {
-#pragma unroll
-    for (int k = 0; k < n; k += 4) {
-      const auto q = load_packed(p + k);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[k + i] = q[i];
-    }
-    return v;
-  }
-#pragma unroll
-  for (int k = 0; k < n; ++k)
-    if (k < count) v[k] = p[k];
-  return v;
-}
-template <typename T>
-__device__ __forceinline__ void store_floats(float* p, Wide<T> v, int count) {
-#pragma unroll
-  for (int k = 0; k < RowTypes<T>::n; ++k)
-    if (k < count) p[k] = v[k];
-}
-template <typename T>
-__device__ __forceinline__ Wide<T> load_gate(const void* gate, int f32, int64_t at, int count) {
-  return f32 ? load_floats<T>(static_cast<const float*>(gate) + at, count)
-             : load_some<T>(static_cast<const T*>(gate) + at, count);
+template <int N, typename T>
+__device__ __forceinline__ Floats<N> load_gate(const void* gate, int f32, int64_t row, unsigned at) {
+  return f32 ? load_elems<N>(static_cast<const float*>(gate) + row + at) : load_elems<N>(static_cast<const T*>(gate) + row + at);
 }
 
-template <typename T>
-__device__ __forceinline__ float dot(Wide<T> a, Wide<T> b, float sum) {
+// A thread's place: a block has S slots of W waves, a slot a row at a time.  `at`: where its i-th N
+// elements start.  The last of a row's vectors is moved back to end with the row; the `again`
+// elements that its neighbour has too are computed by both, alike, and left out of the row's sums.
+template <int N, int W, int NV, int S>
+struct Place {
+  static constexpr int NT = 64 * W;
+  int slot, wave;
+  unsigned tid, at[NV];
+  int again[NV];  // N: the vector is past the row
+  __device__ explicit Place(int dim) {
+    slot = S > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
+    tid = threadIdx.x - slot * NT;
+    wave = __builtin_amdgcn_readfirstlane(tid / 64);
 #pragma unroll
-  for (int k = 0; k < RowTypes<T>::n; ++k) sum = fmaf(a[k], b[k], sum);
+    for (int i = 0; i < NV; ++i) {
+      const int start = ((int)tid + i * NT) * N;
+      again[i] = start + N <= dim ? 0 : start < dim ? start + N - dim : N;
+      at[i] = again[i] == N ? 0 : start - again[i];
+    }
+  }
+  __device__ bool has(int i) const { return again[i] != N; }
+};
+
+// sum + a . b, without the first `again`
+template <int N>
+__device__ __forceinline__ float dot(Floats<N> a, Floats<N> b, float sum, int again) {
+  if (again) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (k >= again) sum = fmaf(a[k], b[k], sum);
+    return sum;
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) sum = fmaf(a[k], b[k], sum);
   return sum;
 }
 
-// The sum over the block, in every thread.  Two calls in a row need W floats of `lds` each of their own:
-// the second one's barrier stands between the first one's reads and the third one's writes.
-template <int W>
-__device__ __forceinline__ float block_sum(float x, float* lds) {
-  x = wave_sum(x);
-  if constexpr (W > 1) {
-    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = x;
-    __syncthreads();
-    x = 0.f;
+// K sums over a slot's W waves at once, in every thread of the slot.  Two calls in a row need `lds` of their own:
+// the second one's barrier, which is the block's, stands between the first one's reads and the third one's
+// writes.
+template <int K, int W>
+__device__ __forceinline__ void slot_sums(float (&x)[K], float (*lds)[K], int wave) {
 #pragma unroll
-    for (int w = 0; w < W; ++w) x += lds[w];
+  for (int k = 0; k < K; ++k) x[k] = wave_sum(x[k]);
+  if constexpr (W > 1) {
+    if (threadIdx.x % 64 == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) lds[wave][k] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int k = 0; k < K; ++k) x[k] += lds[w][k];
   }
-  return x;
 }
 
-template <typename T, int W, int NV>
-__global__ __launch_bounds__(64 * W) void norm_kernel(NormArgs g) {
-  constexpr int N = RowTypes<T>::n, NT = 64 * W;
-  __shared__ float lds[2][W];
-  const int64_t row = block_row();
-  if (row >= g.rows) return;
-  const T* x = static_cast<const T*>(g.x) + row * g.x_stride;
+template <typename T, int N, int W, int NV, int S>
+__global__ __launch_bounds__(64 * W * S) void norm_kernel(NormArgs g) {
+  __shared__ float lds[2][S][W][1];
+  const Place<N, W, NV, S> me(g.dim);
   const float mean = 1.f / (float)g.dim;
-  Wide<T> v[NV], u[NV];
-  int count[NV];
+  Floats<N> weight[NV], post[NV], gate[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int at = ((int)threadIdx.x + i * NT) * N;
-    count[i] = g.dim - at;
-    v[i] = load_some(x + at, count[i]);
-    if (g.y) u[i] = load_some(static_cast<const T*>(g.y) + row * g.y_stride + at, count[i]);
+    weight[i] = post[i] = gate[i] = 1.f;
+    if (!me.has(i)) continue;
+    if (g.weight) weight[i] = load_elems<N>(g.weight + me.at[i]);
+    if (g.post) post[i] = load_elems<N>(g.post + me.at[i]);
   }
-  if (g.y) {
+  int64_t group = -1;
+  int turn = 0;
+  for (int64_t first = block_row() * S; first < g.rows; first += g.row_step) {  // alike in all slots
+    const int64_t row = first + me.slot;
+    const bool there = row < g.rows;
+    Floats<N> v[NV], u[NV];
+    float sum[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      v[i] = u[i] = 0.f;
+      if (!there || !me.has(i)) continue;
+      v[i] = load_elems<N>(static_cast<const T*>(g.x) + row * g.x_stride + me.at[i]);
+      if (g.y) u[i] = load_elems<N>(static_cast<const T*>(g.y) + row * g.y_stride + me.at[i]);
+    }
+    if (there && g.gate && row / g.gate_rows != group) {
+      group = row / g.gate_rows;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (me.has(i)) gate[i] = load_gate<N, T>(g.gate, g.gate_f32, group * g.dim, me.at[i]);
+    }
     float ry = 1.f;
     if (g.post) {
-      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) sum = dot<T>(u[i], u[i], sum);
-      ry = 1.f / sqrtf(block_sum<W>(sum, lds[0]) * mean + g.eps);
+      for (int i = 0; i < NV; ++i) sum[0] = dot<N>(u[i], u[i], sum[0], me.again[i]);
+      slot_sums<1, W>(sum, lds[turn ^= 1][me.slot], me.wave);
+      ry = 1.f / sqrtf(sum[0] * mean + g.eps);
+      sum[0] = 0.f;
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int at = ((int)threadIdx.x + i * NT) * N;
-      if (g.post) u[i] *= ry * load_floats<T>(g.post + at, count[i]);
-      if (g.gate) u[i] *= load_gate<T>(g.gate, g.gate_f32, row / g.gate_rows * g.dim + at, count[i]);
-      v[i] += g.scale * u[i];
-      if (g.x_out) store_some(static_cast<T*>(g.x_out) + row * g.dim + at, v[i], count[i]);
+      v[i] += g.scale * (u[i] * (ry * post[i]) * gate[i]);
+      sum[0] = dot<N>(v[i], v[i], sum[0], me.again[i]);
     }
-    if (g.stats && threadIdx.x == 0) g.stats[row].x = ry;
-  } else if (g.stats && threadIdx.x == 0) {
-    g.stats[row].x = 1.f;
-  }
-  if (!g.h_out && !g.stats) return;
-  float sum = 0.f;
+    slot_sums<1, W>(sum, lds[turn ^= 1][me.slot], me.wave);
+    if (!there) continue;
+    const float rx = 1.f / sqrtf(sum[0] * mean + g.eps);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) sum = dot<T>(v[i], v[i], sum);
-  const float rx = 1.f / sqrtf(block_sum<W>(sum, lds[1]) * mean + g.eps);
-  if (g.stats && threadIdx.x == 0) g.stats[row].y = rx;
-  if (!g.h_out) return;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int at = ((int)threadIdx.x + i * NT) * N;
-    Wide<T> h = v[i] * rx;
-    if (g.weight) h *= load_floats<T>(g.weight + at, count[i]);
-    store_some(static_cast<T*>(g.h_out) + row * g.dim + at, h, count[i]);
+    for (int i = 0; i < NV; ++i) {
+      if (!me.has(i)) continue;
+      if (g.x_out) store_elems<N>(static_cast<T*>(g.x_out) + row * g.dim + me.at[i], v[i]);
+      if (g.h_out) store_elems<N>(static_cast<T*>(g.h_out) + row * g.dim + me.at[i], v[i] * rx * weight[i]);
+    }
+    if (g.stats && me.tid == 0) g.stats[row] = make_float2(ry, rx);
   }
 }
 
-template <typename T, int W, int NV>
-__global__ __launch_bounds__(64 * W) void norm_grad_kernel(NormGradArgs g) {
-  constexpr int N = RowTypes<T>::n, NT = 64 * W;
-  __shared__ float lds[2][W];
-  const int64_t block = block_row();
+// One reduction a row: with k = s gate w_post yh, the sum that dy takes, of k dX, is
+// sum k (dx' + r_x dh w) - r_x mean(dh w xh) sum k xh, so its parts are added up together with sum dh w xh.
+template <typename T, int N, int W, int NV, int S>
+__global__ __launch_bounds__(64 * W * S) void norm_grad_kernel(NormGradArgs g) {
+  constexpr int NT = 64 * W;
+  __shared__ float lds[2][S][W][3];
+  __shared__ float columns[S > 1 ? NV * NT * N : 1];
+  const Place<N, W, NV, S> me(g.dim);
   const NormPlan& p = g.plan;
-  if (block >= p.blocks) return;
+  const int64_t unit = block_row() * S + me.slot;
   const float mean = 1.f / (float)g.dim;
-  int turn = 0;
-  Wide<T> dweight[NV], dpost[NV], dgate[NV];
-  int count[NV];
+  Floats<N> weight[NV], post[NV], gate[NV], dweight[NV], dpost[NV], dgate[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    dweight[i] = dpost[i] = 0.f;
-    count[i] = g.dim - ((int)threadIdx.x + i * NT) * N;
+    weight[i] = post[i] = gate[i] = 1.f;
+    dweight[i] = dpost[i] = dgate[i] = 0.f;
+    if (!me.has(i)) continue;
+    if (g.weight) weight[i] = load_elems<N>(g.weight + me.at[i]);
+    if (g.post) post[i] = load_elems<N>(g.post + me.at[i]);
   }
-  const int64_t group0 = p.segments > 1 ? block / p.segments : block * p.per_block;
-  int64_t group1 = p.segments > 1 ? group0 + 1 : group0 + p.per_block;
-  if (group1 > p.groups) group1 = p.groups;
-  for (int64_t group = group0; group < group1; ++group) {
-    const int64_t first = group * p.span;
-    const int64_t from = first + (p.segments > 1 ? block % p.segments * p.seg_rows : 0);
-    int64_t to = from + p.seg_rows;
-    if (to > first + p.span) to = first + p.span;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) dgate[i] = 0.f;
-    for (int64_t row = from; row < to; ++row) {
-      const float2 r = g.stats[row];
-      Wide<T> d[NV], a[NV], b[NV];
-      float sum = 0.f;
+  const int64_t from = p.segments > 1 ? unit / p.segments * p.span + unit % p.segments * p.unit_rows : unit * p.unit_rows;
+  int64_t to = from + p.unit_rows;
+  if (p.segments > 1 && to > (unit / p.segments + 1) * p.span) to = (unit / p.segments + 1) * p.span;
+  if (to > g.rows) to = g.rows;
+  if (unit >= p.units) to = from;
+  int64_t in_group = 0, group = p.segments > 1 ? unit / p.segments : from / p.span;
+  for (int64_t it = 0; it < p.unit_rows; ++it) {  // alike in all slots: the reductions are the block's
+    const int64_t row = from + it;
+    const bool there = row < to;
+    Floats<N> d[NV], a[NV], b[NV], y[NV];
+    float2 r = make_float2(0.f, 0.f);
+    float sums[3] = {0.f, 0.f, 0.f};
+    if (there) {
+      r = g.stats[row];
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int at = ((int)threadIdx.x + i * NT) * N;
-        d[i] = 0.f;
-        if (g.dx) d[i] = load_some(static_cast<const T*>(g.dx) + row * g.dx_stride + at, count[i]);
+        d[i] = a[i] = b[i] = y[i] = 0.f;
+        if (!me.has(i)) continue;
+        if (g.dx) d[i] = load_elems<N>(static_cast<const T*>(g.dx) + row * g.dx_stride + me.at[i]);
         if (g.dh) {
-          a[i] = r.y * load_some(static_cast<const T*>(g.x) + row * g.x_stride + at, count[i]);
-          b[i] = load_some(static_cast<const T*>(g.dh) + row * g.dh_stride + at, count[i]);
-          dweight[i] += b[i] * a[i];
-          if (g.weight) b[i] *= load_floats<T>(g.weight + at, count[i]);
-          sum = dot<T>(a[i], b[i], sum);
+          a[i] = load_elems<N>(static_cast<const T*>(g.x) + row * g.x_stride + me.at[i]);
+          b[i] = load_elems<N>(static_cast<const T*>(g.dh) + row * g.dh_stride + me.at[i]);
         }
-      }
-      if (g.dh) {
-        sum = block_sum<W>(sum, lds[turn ^= 1]) * mean;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) d[i] += r.y * (b[i] - a[i] * sum);
+        if (g.y) y[i] = load_elems<N>(static_cast<const T*>(g.y) + row * g.y_stride + me.at[i]);
+        if (g.gate && in_group == 0) gate[i] = load_gate<N, T>(g.gate, g.gate_f32, group * g.dim, me.at[i]);
       }
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int at = ((int)threadIdx.x + i * NT) * N;
-        if (g.grad_x) store_some(static_cast<T*>(g.grad_x) + row * g.dim + at, d[i], count[i]);
-      }
-      if (!g.y) continue;
-      sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int at = ((int)threadIdx.x + i * NT) * N;
-        a[i] = load_some(static_cast<const T*>(g.y) + row * g.y_stride + at, count[i]);
-        if (g.post) a[i] *= r.x;
-        d[i] *= g.scale;
-        Wide<T> post = 1.f;
-        if (g.post) post = load_floats<T>(g.post + at, count[i]);
-        if (g.gate) {
-          dgate[i] += d[i] * a[i] * post;
-          d[i] *= load_gate<T>(g.gate, g.gate_f32, group * g.dim + at, count[i]);
-        }
+        a[i] *= r.y;
+        dweight[i] += b[i] * a[i];
+        b[i] *= weight[i];
+        sums[0] = dot<N>(a[i], b[i], sums[0], me.again[i]);
+        d[i] += r.y * b[i];
+        y[i] *= r.x;
         if (g.post) {
-          dpost[i] += d[i] * a[i];
-          d[i] *= post;
-          sum = dot<T>(d[i], a[i], sum);
+          const Floats<N> k = y[i] * post[i] * gate[i];
+          sums[1] = dot<N>(k, d[i], sums[1], me.again[i]);
+          sums[2] = dot<N>(k, a[i], sums[2], me.again[i]);
         }
       }
-      if (g.post) sum = block_sum<W>(sum, lds[turn ^= 1]) * mean;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int at = ((int)threadIdx.x + i * NT) * N;
-        if (g.post) d[i] = r.x * (d[i] - a[i] * sum);
-        if (g.grad_y) store_some(static_cast<T*>(g.grad_y) + row * g.dim + at, d[i], count[i]);
-      }
     }
-    if (g.grad_gate) {
+    slot_sums<3, W>(sums, lds[it & 1][me.slot], me.wave);
+    if (!there) continue;
+    const float inner = r.y * sums[0] * mean, outer = g.post ? g.scale * (sums[1] - inner * sums[2]) * mean : 0.f;
+    const bool last = ++in_group == p.span || row + 1 == to;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int at = ((int)threadIdx.x + i * NT) * N;
-        if (p.segments > 1) store_floats<T>(g.partial + (2 * p.blocks + block) * g.dim + at, dgate[i], count[i]);
-        else if (g.gate_f32) store_floats<T>(static_cast<float*>(g.grad_gate) + group * g.dim + at, dgate[i], count[i]);
-        else store_some(static_cast<T*>(g.grad_gate) + group * g.dim + at, dgate[i], count[i]);
-      }
+    for (int i = 0; i < NV; ++i) {
+      d[i] -= inner * a[i];
+      if (g.grad_x && me.has(i)) store_elems<N>(static_cast<T*>(g.grad_x) + row * g.dim + me.at[i], d[i]);
+      if (!g.y) continue;
+      d[i] *= g.scale;
+      dgate[i] += d[i] * y[i] * post[i];
+      d[i] *= gate[i];
+      dpost[i] += d[i] * y[i];
+      if (g.grad_y && me.has(i))
+        store_elems<N>(static_cast<T*>(g.grad_y) + row * g.dim + me.at[i], r.x * (d[i] * post[i] - y[i] * outer));
     }
-  }
+    if (!last || p.groups == 1) continue;
+    in_group = 0;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int at = ((int)threadIdx.x + i * NT) * N;
-    if (g.grad_weight) store_floats<T>(g.partial + block * g.dim + at, dweight[i], count[i]);
-    if (g.grad_post) store_floats<T>(g.partial + (p.blocks + block) * g.dim + at, dpost[i], count[i]);
+    for (int i = 0; i < NV; ++i) {
+      if (g.grad_gate && me.has(i)) {
+        if (p.segments > 1) store_elems<N>(g.partial + (2 * p.blocks + unit) * g.dim + me.at[i], dgate[i]);
+        else if (g.gate_f32) store_elems<N>(static_cast<float*>(g.grad_gate) + group * g.dim + me.at[i], dgate[i]);
+        else store_elems<N>(static_cast<T*>(g.grad_gate) + group * g.dim + me.at[i], dgate[i]);
+      }
+      dgate[i] = 0.f;
+    }
+    ++group;
   }
+  // the slots' sums over rows, added one after the other, then the block's to the workspace
+  auto out = [&](Floats<N>(&sum)[NV], float* to) {
+    if constexpr (S > 1) {
+      for (int k = 0; k < S; ++k) {
+        __syncthreads();
+        if (me.slot == k)
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+              float& c = columns[(i * N + e) * NT + me.tid];
+              sum[i][e] = k ? c + sum[i][e] : sum[i][e];
+              c = sum[i][e];
+            }
+      }
+      if (me.slot != S - 1) return;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (me.has(i)) store_elems<N>(to + me.at[i], sum[i]);
+  };
+  const int64_t block = block_row();
+  if (block >= p.blocks) return;
+  if (g.grad_weight) out(dweight, g.partial + block * g.dim);
+  if (g.grad_post) out(dpost, g.partial + (p.blocks + block) * g.dim);
+  if (g.grad_gate && p.groups == 1) out(dgate, g.partial + (2 * p.blocks + block) * g.dim);
 }
 
 // The blocks' sums added in a fixed order: blockIdx.y 0 the weights', 1 the post norm's, 2 + group a
 // group's vector of the gate.
+constexpr int kSumWaves = 16;
 template <typename G>
-__global__ __launch_bounds__(256) void norm_sums_kernel(NormGradArgs g) {
-  __shared__ float lds[4][64];
+__global__ __launch_bounds__(64 * kSumWaves) void norm_sums_kernel(NormGradArgs g) {
+  __shared__ float lds[kSumWaves][64];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, column = (int)blockIdx.x * 64 + lane;
   const int64_t which = blockIdx.y, group = which - 2;
   if (which == 0 ? !g.grad_weight : which == 1 && !g.grad_post) return;
-  const int64_t count = which < 2 ? g.plan.blocks : g.plan.segments;
+  const int64_t count = which < 2 || g.plan.groups == 1 ? g.plan.blocks : g.plan.segments;
   const float* p = g.partial + (which < 2 ? which * count : 2 * g.plan.blocks + group * count) * g.dim + column;
   float sum = 0.f;
   if (column < g.dim)
-    for (int64_t k = wave; k < count; k += 4) sum += p[k * g.dim];
+#pragma unroll 8
+    for (int64_t k = wave; k < count; k += kSumWaves) sum += p[k * g.dim];
   lds[wave][lane] = sum;
   __syncthreads();
   if (wave != 0 || column >= g.dim) return;
-  sum = (lds[0][lane] + lds[1][lane]) + (lds[2][lane] + lds[3][lane]);
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kSumWaves; ++w) sum += lds[w][lane];
   if (which == 0) g.grad_weight[column] = sum;
   else if (which == 1) g.grad_post[column] = sum;
   else static_cast<G*>(g.grad_gate)[group * g.dim + column] = (G)sum;
 }
 
-// The threads and vectors each that hold a row of `dim` elements.
+// Waves a row, with 8 elements a thread while a block's 16 waves reach; row slots fill them up.
+int norm_waves(int64_t dim) {
+  static const int waves[] = {1, 2, 4, 6, 8, 10, 12};
+  for (int w : waves)
+    if (dim <= 512 * w) return w;
+  return 16;
+}
+
 template <typename T, typename F>
 void by_dim(int dim, F f) {
-  const int vectors = (dim + RowTypes<T>::n - 1) / RowTypes<T>::n;
   using std::integral_constant;
-#define HVDX_SHAPE(w, nv) f(integral_constant<int, w>{}, integral_constant<int, nv>{})
-  if (vectors <= 64) HVDX_SHAPE(1, 1);
-  else if (vectors <= 128) HVDX_SHAPE(1, 2);
-  else if (vectors <= 256) HVDX_SHAPE(4, 1);
-  else if (vectors <= 512) HVDX_SHAPE(4, 2);
-  else if (vectors <= 1024) HVDX_SHAPE(16, 1);
-  else if (vectors <= 2048) HVDX_SHAPE(16, 2);
-  else if (vectors <= 4096) HVDX_SHAPE(16, 4);
-  else if constexpr (sizeof(T) == 4) HVDX_SHAPE(16, 8);
+  constexpr int N = RowTypes<T>::n, NV = 8 / N;
+#define HVDX_SHAPE(n, w, nv) f(integral_constant<int, n>{}, integral_constant<int, w>{}, integral_constant<int, nv>{})
+  if (dim < N) HVDX_SHAPE(1, 1, 1);  // a row in fewer than 64 lanes, an element each
+  else switch (norm_waves(dim)) {
+    case 1: HVDX_SHAPE(N, 1, NV); break;
+    case 2: HVDX_SHAPE(N, 2, NV); break;
+    case 4: HVDX_SHAPE(N, 4, NV); break;
+    case 6: HVDX_SHAPE(N, 6, NV); break;
+    case 8: HVDX_SHAPE(N, 8, NV); break;
+    case 10: HVDX_SHAPE(N, 10, NV); break;
+    case 12: HVDX_SHAPE(N, 12, NV); break;
+    default:
+      if (dim <= 8 * 1024) HVDX_SHAPE(N, 16, NV);
+      else if (dim <= 16 * 1024) HVDX_SHAPE(N, 16, 2 * NV);
+      else HVDX_SHAPE(N, 16, 4 * NV);
+  }
 #undef HVDX_SHAPE
 }
-static_assert(HVDX_MAX_NORM_DIM <= 64 * 16 * 8 * 4 && HVDX_MAX_NORM_DIM <= 64 * 16 * 4 * 8);
+static_assert(HVDX_MAX_NORM_DIM <= 32 * 1024);
+constexpr int slots_of(int waves) { return 16 / waves; }
 
 }  // namespace
 
-hipError_t launch_norm(const NormArgs& g, int dtype, hipStream_t stream) {
+hipError_t launch_norm(const NormArgs& args, int dtype, hipStream_t stream) {
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    by_dim<T>(g.dim, [&](auto w, auto nv) {
-      HVDX_LAUNCH((norm_kernel<T, w(), nv()>), row_grid(g.rows), dim3(64 * w()), 0, stream, g);
+    by_dim<T>(args.dim, [&](auto n, auto w, auto nv) {
+      // a slot a row while rows are few; a block's slots take turns once there are more than the chip holds
+      constexpr int W = w(), S = W >= 4 ? 1 : 4 / W;
+      NormArgs g = args;
+      int64_t blocks = (g.rows + S - 1) / S;
+      const int64_t most = 256 * (32 / (W * S));
+      if (blocks > most) blocks = most;
+      g.row_step = blocks * S;
+      HVDX_LAUNCH((norm_kernel<T, n(), W, nv(), S>), row_grid(blocks), dim3(64 * W * S), 0, stream, g);
     });
   });
   return hipGetLastError();
 }
 
-NormPlan norm_plan(int64_t rows, int64_t gate_rows) {
-  constexpr int64_t kBlocks = 512;
+NormPlan norm_plan(int64_t rows, int64_t dim, int64_t gate_rows) {
+  const int slots = slots_of(norm_waves(dim));
+  const int64_t units = 256 * slots;  // a block for each compute unit
   NormPlan p{};
   p.span = gate_rows ? gate_rows : rows;
   p.groups = rows / p.span;
   p.segments = 1;
-  if (p.groups < kBlocks) p.segments = (kBlocks + p.groups - 1) / p.groups;
+  if (p.groups < units) p.segments = (units + p.groups - 1) / p.groups;
   if (p.segments > p.span) p.segments = p.span;
-  p.seg_rows = (p.span + p.segments - 1) / p.segments;
-  p.segments = (p.span + p.seg_rows - 1) / p.seg_rows;
-  p.per_block = p.segments > 1 ? 1 : (p.groups + kBlocks - 1) / kBlocks;
-  p.blocks = p.segments > 1 ? p.groups * p.segments : (p.groups + p.per_block - 1) / p.per_block;
+  p.unit_rows = (p.span + p.segments - 1) / p.segments;
+  p.segments = (p.span + p.unit_rows - 1) / p.unit_rows;
+  if (p.segments == 1) {
+    const int64_t whole = (p.groups + units - 1) / units;  // groups a unit
+    p.unit_rows = whole * p.span;
+    p.units = (p.groups + whole - 1) / whole;
+  } else {
+    p.units = p.groups * p.segments;
+  }
+  p.blocks = (p.units + slots - 1) / slots;
   return p;
 }
 
 hipError_t launch_norm_grad(const NormGradArgs& g, int dtype, hipStream_t stream) {
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    by_dim<T>(g.dim, [&](auto w, auto nv) {
-      HVDX_LAUNCH((norm_grad_kernel<T, w(), nv()>), row_grid(g.plan.blocks), dim3(64 * w()), 0, stream, g);
+    by_dim<T>(g.dim, [&](auto n, auto w, auto nv) {
+      constexpr int W = w(), S = slots_of(W);
+      HVDX_LAUNCH((norm_grad_kernel<T, n(), W, nv(), S>), row_grid(g.plan.blocks), dim3(64 * W * S), 0, stream, g);
     });
   });
   return hipGetLastError();
 }
 
 hipError_t launch_norm_grad_sums(const NormGradArgs& g, int dtype, hipStream_t stream) {
-  const int64_t gates = g.grad_gate && g.plan.segments > 1 ? g.plan.groups : 0;  // fewer than norm_plan's blocks
+  const int64_t gates = g.grad_gate && norm_gate_partials(g.plan) ? g.plan.groups : 0;  // fewer than norm_plan's units
   const dim3 grid((unsigned)(g.dim + 63) / 64, (unsigned)(2 + gates));
   by_type(g.gate_f32 ? HVDX_FLOAT32 : dtype, [&](auto t) {
-    HVDX_LAUNCH(norm_sums_kernel<decltype(t)>, grid, dim3(256), 0, stream, g);
+    HVDX_LAUNCH(norm_sums_kernel<decltype(t)>, grid, dim3(64 * kSumWaves), 0, stream, g);
   });
   return hipGetLastError();
 }
