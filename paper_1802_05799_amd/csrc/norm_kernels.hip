@@ -32,6 +32,16 @@ __device__ __forceinline__ Floats<N> load_elems(const T* p) {
   const typename Elems<T, N>::packed v = *reinterpret_cast<const typename Elems<T, N>::raw*>(p);
   return __builtin_convertvector(v, Floats<N>);
 }
+// Rows are read once: past the caches (4 to 9% faster than through them at 0.3 to 1 GB; results are
+// stored through them, for what reads them next).
+template <int N, typename T>
+__device__ __forceinline__ typename Elems<T, N>::packed stream_packed(const T* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const typename Elems<T, N>::raw*>(p));
+}
+template <int N, typename T>
+__device__ __forceinline__ Floats<N> stream_elems(const T* p) {
+  return __builtin_convertvector(stream_packed<N>(p), Floats<N>);
+}
 template <int N, typename T>
 __device__ __forceinline__ void store_elems(T* p, Floats<N> v) {
   *reinterpret_cast<typename Elems<T, N>::raw*>(p) = __builtin_convertvector(v, typename Elems<T, N>::packed);
@@ -90,12 +100,9 @@ __device__ __forceinline__ void slot_sums(float (&x)[K], float (*lds)[K], int wa
 #pragma unroll
       for (int k = 0; k < K; ++k) lds[wave][k] = x[k];
     __syncthreads();
+    const int lane = threadIdx.x % 64;
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = 0.f;
-#pragma unroll
-    for (int w = 0; w < W; ++w)
-#pragma unroll
-      for (int k = 0; k < K; ++k) x[k] += lds[w][k];
+    for (int k = 0; k < K; ++k) x[k] = wave_sum(lane < W ? lds[lane][k] : 0.f);
   }
 }
 
@@ -123,8 +130,8 @@ __global__ __launch_bounds__(64 * W * S) void norm_kernel(NormArgs g) {
     for (int i = 0; i < NV; ++i) {
       v[i] = u[i] = 0.f;
       if (!there || !me.has(i)) continue;
-      v[i] = load_elems<N>(static_cast<const T*>(g.x) + row * g.x_stride + me.at[i]);
-      if (g.y) u[i] = load_elems<N>(static_cast<const T*>(g.y) + row * g.y_stride + me.at[i]);
+      v[i] = stream_elems<N>(static_cast<const T*>(g.x) + row * g.x_stride + me.at[i]);
+      if (g.y) u[i] = stream_elems<N>(static_cast<const T*>(g.y) + row * g.y_stride + me.at[i]);
     }
     if (there && g.gate && row / g.gate_rows != group) {
       group = row / g.gate_rows;
@@ -158,25 +165,65 @@ __global__ __launch_bounds__(64 * W * S) void norm_kernel(NormArgs g) {
   }
 }
 
+// A row's four inputs as they lie: 0 where one is not there.
+template <typename T, int N, int NV>
+struct GradRow {
+  typename Elems<T, N>::packed dx[NV], x[NV], dh[NV], y[NV];
+  float2 r;
+  template <typename P>
+  __device__ __forceinline__ void load(const NormGradArgs& g, const P& me, int64_t row) {
+    r = g.stats[row];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      dx[i] = x[i] = dh[i] = y[i] = (T)0.f;
+      if (!me.has(i)) continue;
+      if (g.dx) dx[i] = stream_packed<N>(static_cast<const T*>(g.dx) + row * g.dx_stride + me.at[i]);
+      if (g.dh) {
+        x[i] = stream_packed<N>(static_cast<const T*>(g.x) + row * g.x_stride + me.at[i]);
+        dh[i] = stream_packed<N>(static_cast<const T*>(g.dh) + row * g.dh_stride + me.at[i]);
+      }
+      if (g.y) y[i] = stream_packed<N>(static_cast<const T*>(g.y) + row * g.y_stride + me.at[i]);
+    }
+  }
+};
+
 // One reduction a row: with k = s gate w_post yh, the sum that dy takes, of k dX, is
 // sum k (dx' + r_x dh w) - r_x mean(dh w xh) sum k xh, so its parts are added up together with sum dh w xh.
-template <typename T, int N, int W, int NV, int S>
+//
+// All slots reduce at the same time, so the next row is loaded before the reduction (AHEAD).  The registers for
+// that come from keeping a row as it lies, and from the sums over rows being in LDS (LSUMS of the three; a
+// thread's own places, 16 bytes an access): 98 KB of the 160 for 1024 threads of 8 elements.  Longer rows
+// leave room for less: no row ahead, the weights from the caches for every row (HELD false).
+template <typename T, int N, int W, int NV, int S, bool AHEAD, bool HELD, int LSUMS>
 __global__ __launch_bounds__(64 * W * S) void norm_grad_kernel(NormGradArgs g) {
   constexpr int NT = 64 * W;
   __shared__ float lds[2][S][W][3];
-  __shared__ float columns[S > 1 ? NV * NT * N : 1];
+  __shared__ Floats<N> held[LSUMS][NV][NT * S];
   const Place<N, W, NV, S> me(g.dim);
   const NormPlan& p = g.plan;
   const int64_t unit = block_row() * S + me.slot;
   const float mean = 1.f / (float)g.dim;
-  Floats<N> weight[NV], post[NV], gate[NV], dweight[NV], dpost[NV], dgate[NV];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    weight[i] = post[i] = gate[i] = 1.f;
-    dweight[i] = dpost[i] = dgate[i] = 0.f;
-    if (!me.has(i)) continue;
+  Floats<N> weight[NV], post[NV], gate[NV], sum[3 - LSUMS + 1][NV];
+  // sums over rows: 0 the weight's, 1 the post norm's, 2 the gate's
+  auto total = [&](int which, int i) -> Floats<N>& {
+    if (which < LSUMS) return held[which][i][threadIdx.x];
+    return sum[which - LSUMS][i];
+  };
+  auto weights = [&](int i) {
+    weight[i] = post[i] = 1.f;
+    if (!me.has(i)) return;
     if (g.weight) weight[i] = load_elems<N>(g.weight + me.at[i]);
     if (g.post) post[i] = load_elems<N>(g.post + me.at[i]);
+  };
+  auto gates = [&](int i, int64_t group) {
+    gate[i] = 1.f;
+    if (g.gate && me.has(i)) gate[i] = load_gate<N, T>(g.gate, g.gate_f32, group * g.dim, me.at[i]);
+  };
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    if constexpr (HELD) weights(i);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) total(k, i) = 0.f;
   }
   const int64_t from = p.segments > 1 ? unit / p.segments * p.span + unit % p.segments * p.unit_rows : unit * p.unit_rows;
   int64_t to = from + p.unit_rows;
@@ -184,96 +231,85 @@ __global__ __launch_bounds__(64 * W * S) void norm_grad_kernel(NormGradArgs g) {
   if (to > g.rows) to = g.rows;
   if (unit >= p.units) to = from;
   int64_t in_group = 0, group = p.segments > 1 ? unit / p.segments : from / p.span;
+  GradRow<T, N, NV> now, next;
+  if (AHEAD && from < to) next.load(g, me, from);
   for (int64_t it = 0; it < p.unit_rows; ++it) {  // alike in all slots: the reductions are the block's
     const int64_t row = from + it;
     const bool there = row < to;
-    Floats<N> d[NV], a[NV], b[NV], y[NV];
-    float2 r = make_float2(0.f, 0.f);
     float sums[3] = {0.f, 0.f, 0.f};
     if (there) {
-      r = g.stats[row];
+      if constexpr (AHEAD) now = next;
+      else now.load(g, me, row);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        d[i] = a[i] = b[i] = y[i] = 0.f;
-        if (!me.has(i)) continue;
-        if (g.dx) d[i] = load_elems<N>(static_cast<const T*>(g.dx) + row * g.dx_stride + me.at[i]);
-        if (g.dh) {
-          a[i] = load_elems<N>(static_cast<const T*>(g.x) + row * g.x_stride + me.at[i]);
-          b[i] = load_elems<N>(static_cast<const T*>(g.dh) + row * g.dh_stride + me.at[i]);
-        }
-        if (g.y) y[i] = load_elems<N>(static_cast<const T*>(g.y) + row * g.y_stride + me.at[i]);
-        if (g.gate && in_group == 0) gate[i] = load_gate<N, T>(g.gate, g.gate_f32, group * g.dim, me.at[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        a[i] *= r.y;
-        dweight[i] += b[i] * a[i];
-        b[i] *= weight[i];
-        sums[0] = dot<N>(a[i], b[i], sums[0], me.again[i]);
-        d[i] += r.y * b[i];
-        y[i] *= r.x;
+        if constexpr (!HELD) weights(i);
+        if (!HELD || in_group == 0) gates(i, group);
+        const Floats<N> a = __builtin_convertvector(now.x[i], Floats<N>) * now.r.y, dh = __builtin_convertvector(now.dh[i], Floats<N>);
+        total(0, i) += dh * a;
+        const Floats<N> b = dh * weight[i];
+        sums[0] = dot<N>(a, b, sums[0], me.again[i]);
         if (g.post) {
-          const Floats<N> k = y[i] * post[i] * gate[i];
-          sums[1] = dot<N>(k, d[i], sums[1], me.again[i]);
-          sums[2] = dot<N>(k, a[i], sums[2], me.again[i]);
+          const Floats<N> k = __builtin_convertvector(now.y[i], Floats<N>) * now.r.x * post[i] * gate[i];
+          sums[1] = dot<N>(k, __builtin_convertvector(now.dx[i], Floats<N>) + now.r.y * b, sums[1], me.again[i]);
+          sums[2] = dot<N>(k, a, sums[2], me.again[i]);
         }
       }
+      if (AHEAD && row + 1 < to) next.load(g, me, row + 1);
     }
     slot_sums<3, W>(sums, lds[it & 1][me.slot], me.wave);
     if (!there) continue;
-    const float inner = r.y * sums[0] * mean, outer = g.post ? g.scale * (sums[1] - inner * sums[2]) * mean : 0.f;
+    const float inner = now.r.y * sums[0] * mean, outer = g.post ? g.scale * (sums[1] - inner * sums[2]) * mean : 0.f;
     const bool last = ++in_group == p.span || row + 1 == to;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      d[i] -= inner * a[i];
-      if (g.grad_x && me.has(i)) store_elems<N>(static_cast<T*>(g.grad_x) + row * g.dim + me.at[i], d[i]);
+      if constexpr (!HELD) {
+        weights(i);
+        gates(i, group);
+      }
+      const Floats<N> a = __builtin_convertvector(now.x[i], Floats<N>) * now.r.y;
+      Floats<N> d = __builtin_convertvector(now.dx[i], Floats<N>) + now.r.y * (__builtin_convertvector(now.dh[i], Floats<N>) * weight[i]);
+      d -= inner * a;
+      if (g.grad_x && me.has(i)) store_elems<N>(static_cast<T*>(g.grad_x) + row * g.dim + me.at[i], d);
       if (!g.y) continue;
-      d[i] *= g.scale;
-      dgate[i] += d[i] * y[i] * post[i];
-      d[i] *= gate[i];
-      dpost[i] += d[i] * y[i];
+      const Floats<N> y = __builtin_convertvector(now.y[i], Floats<N>) * now.r.x;
+      d *= g.scale;
+      if (g.gate) total(2, i) += d * y * post[i];
+      d *= gate[i];
+      if (g.post) total(1, i) += d * y;
       if (g.grad_y && me.has(i))
-        store_elems<N>(static_cast<T*>(g.grad_y) + row * g.dim + me.at[i], r.x * (d[i] * post[i] - y[i] * outer));
+        store_elems<N>(static_cast<T*>(g.grad_y) + row * g.dim + me.at[i], now.r.x * (d * post[i] - y * outer));
     }
     if (!last || p.groups == 1) continue;
     in_group = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (g.grad_gate && me.has(i)) {
-        if (p.segments > 1) store_elems<N>(g.partial + (2 * p.blocks + unit) * g.dim + me.at[i], dgate[i]);
-        else if (g.gate_f32) store_elems<N>(static_cast<float*>(g.grad_gate) + group * g.dim + me.at[i], dgate[i]);
-        else store_elems<N>(static_cast<T*>(g.grad_gate) + group * g.dim + me.at[i], dgate[i]);
+        if (p.segments > 1) store_elems<N>(g.partial + (2 * p.blocks + unit) * g.dim + me.at[i], total(2, i));
+        else if (g.gate_f32) store_elems<N>(static_cast<float*>(g.grad_gate) + group * g.dim + me.at[i], total(2, i));
+        else store_elems<N>(static_cast<T*>(g.grad_gate) + group * g.dim + me.at[i], total(2, i));
       }
-      dgate[i] = 0.f;
+      total(2, i) = 0.f;
     }
     ++group;
   }
-  // the slots' sums over rows, added one after the other, then the block's to the workspace
-  auto out = [&](Floats<N>(&sum)[NV], float* to) {
-    if constexpr (S > 1) {
-      for (int k = 0; k < S; ++k) {
-        __syncthreads();
-        if (me.slot == k)
-#pragma unroll
-          for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-              float& c = columns[(i * N + e) * NT + me.tid];
-              sum[i][e] = k ? c + sum[i][e] : sum[i][e];
-              c = sum[i][e];
-            }
-      }
-      if (me.slot != S - 1) return;
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (me.has(i)) store_elems<N>(to + me.at[i], sum[i]);
-  };
+  // the slots' sums over rows, added in their order, then the block's to the workspace
   const int64_t block = block_row();
   if (block >= p.blocks) return;
-  if (g.grad_weight) out(dweight, g.partial + block * g.dim);
-  if (g.grad_post) out(dpost, g.partial + (p.blocks + block) * g.dim);
-  if (g.grad_gate && p.groups == 1) out(dgate, g.partial + (2 * p.blocks + block) * g.dim);
+  __syncthreads();
+  if (me.slot > 0) return;
+  auto out = [&](int which, float* to) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      Floats<N> v = total(which, i);
+      if constexpr (S > 1)
+        for (int k = 1; k < S; ++k) v += held[which][i][threadIdx.x + k * NT];
+      if (me.has(i)) store_elems<N>(to + me.at[i], v);
+    }
+  };
+  static_assert(S == 1 || LSUMS == 3);
+  if (g.grad_weight) out(0, g.partial + block * g.dim);
+  if (g.grad_post) out(1, g.partial + (p.blocks + block) * g.dim);
+  if (g.grad_gate && p.groups == 1) out(2, g.partial + (2 * p.blocks + block) * g.dim);
 }
 
 // The blocks' sums added in a fixed order: blockIdx.y 0 the weights', 1 the post norm's, 2 + group a
@@ -379,8 +415,10 @@ hipError_t launch_norm_grad(const NormGradArgs& g, int dtype, hipStream_t stream
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
     by_dim<T>(g.dim, [&](auto n, auto w, auto nv) {
-      constexpr int W = w(), S = slots_of(W);
-      HVDX_LAUNCH((norm_grad_kernel<T, n(), W, nv(), S>), row_grid(g.plan.blocks), dim3(64 * W * S), 0, stream, g);
+      constexpr int N = n(), W = w(), NV = nv(), S = slots_of(W), elements = N * NV;
+      constexpr bool held = elements <= 8, ahead = held && (sizeof(T) == 2 || W * S < 16);  // there are registers for it
+      HVDX_LAUNCH((norm_grad_kernel<T, N, W, NV, S, ahead, held, elements <= 8 ? 3 : elements <= 16 ? 2 : 1>),
+                  row_grid(g.plan.blocks), dim3(64 * W * S), 0, stream, g);
     });
   });
   return hipGetLastError();

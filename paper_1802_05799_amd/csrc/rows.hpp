@@ -62,17 +62,27 @@ __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
+// f over a wavefront's 64 values, in every lane: within rows of 16 lanes by shifts, then from row to row, the result
+// out of the last lane.  `none` is what f leaves alone.
+template <int CONTROL, int ROWS, typename F>
+__device__ __forceinline__ float lanes_step(float x, float none, F f) {
+  return f(x, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(x), CONTROL, ROWS, 0xf, false)));
+}
 template <typename F>
-__device__ __forceinline__ float wave_reduce(float x, F f) {
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) x = f(x, __shfl_xor(x, k));
-  return x;
+__device__ __forceinline__ float wave_reduce(float x, float none, F f) {
+  x = lanes_step<0x111, 0xf>(x, none, f);  // from 1, 2, 4 and 8 lanes below
+  x = lanes_step<0x112, 0xf>(x, none, f);
+  x = lanes_step<0x114, 0xf>(x, none, f);
+  x = lanes_step<0x118, 0xf>(x, none, f);
+  x = lanes_step<0x142, 0xa>(x, none, f);  // the last lane of a row to the next row
+  x = lanes_step<0x143, 0xc>(x, none, f);  // lane 31 to the upper half
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 __device__ __forceinline__ float wave_sum(float x) {
-  return wave_reduce(x, [](float a, float b) { return a + b; });
+  return wave_reduce(x, 0.f, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float wave_max(float x) {
-  return wave_reduce(x, [](float a, float b) { return fmaxf(a, b); });
+  return wave_reduce(x, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
 }
 
 // A block for each row; grids are two-dimensional, as a dimension has fewer than 2^32 threads.
