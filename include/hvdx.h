@@ -615,7 +615,7 @@ int hvdx_token_logprobs_grad(const void* logits, int64_t stride, int dtype, int6
  *   loss[rows]     float, out (NULL where not wanted).  A row without entries has loss 0 (and gradient 0).  It
  *                  is infinite where the student gives a token of positive q no probability; a q_R of at
  *                  most 1e-6 then counts as the rounding of 0
- *   stats[rows*4]  float, out, 16-byte aligned: what hvdx_distill_grad takes; NULL where not wanted
+ *   stats[rows*8]  float, out, 16-byte aligned: what hvdx_distill_grad takes
  *   grad           out, NULL where not wanted: d/dz of sum over rows of grad_loss[row] loss, of the logits' type, its
  *                  row stride grad_stride; may be logits.  Takes grad_loss ([rows] float)
  *   workspace      hvdx_distill_workspace_bytes(rows, vocab) bytes, as above

@@ -258,7 +258,7 @@ struct LogprobArgs {
   int top;
   int64_t* top_ids;
   float* top_logprobs;
-  float4* stats;  // row's maximum, log of its sum, entropy
+  float4* stats;  // reference, log2 of the sum, entropy, 1 where the reference is unscaled
   int parts;      // blocks a row (row_parts); with more than one:
   float4* part_sums;    // [rows][parts]
   uint64_t* part_keys;  // [rows][parts][top]
@@ -276,8 +276,15 @@ struct LogprobGradArgs {
   const float *grad_logprob, *grad_entropy;
   void* grad;
   int64_t grad_stride;
+  int64_t chunks;  // blocks a row, set by the launch
 };
 hipError_t launch_logprobs_grad(const LogprobGradArgs& g, int dtype, hipStream_t stream);
+struct alignas(16) DistillStats {
+  float rest_ref, f;       // reference of the sum over unlisted (or all) tokens, the factor of their gradient
+  float ref, log2s, total;  // the row's reference and log2 of its sum, the teacher's mass
+  float wide;              // 1 where the references are unscaled
+  float pad0, pad1;
+};
 struct DistillArgs {
   const void* logits;
   int64_t stride, rows;
@@ -288,10 +295,16 @@ struct DistillArgs {
   int entries, rest;
   const float* grad_loss;
   float* loss;
-  float4* stats;  // maximum of what the sum is over, its gradient's factor, the row's maximum and log of its sum
+  DistillStats* stats;
   void* grad;
   int64_t grad_stride;
+  int parts;          // blocks a row; with more than one:
+  float4* part_sums;  // [rows][parts]
+  int64_t chunks;     // blocks a row of the gradient, set by the launch
 };
+// Parts of a row (1: with `grad`, the launch writes the gradient too; else join and grad launches follow).
+int distill_parts(int64_t rows, int64_t vocab, int dtype, bool grad);
+hipError_t launch_distill_join(const DistillArgs& g, int dtype, hipStream_t stream);
 hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream);
 hipError_t launch_distill_grad(const DistillArgs& g, int dtype, hipStream_t stream);
 

@@ -177,7 +177,7 @@ int hvdx_token_logprobs_grad(const void* logits, int64_t stride, int dtype, int6
   const unsigned same[1] = {1};
   if (int rc = check_buffers(in, 5, out, 1, same, what)) return rc;
   const hvdx::LogprobGradArgs g{logits, stride, rows, (int)vocab, scale, tokens, reinterpret_cast<const float4*>(stats),
-                                grad_logprob, grad_entropy, grad, grad_stride};
+                                grad_logprob, grad_entropy, grad, grad_stride, 0};
   const hipStream_t st = static_cast<hipStream_t>(stream);
   TimedLaunch phase(HVDX_KERNEL_LOGPROBS_GRAD, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
   return launched(timed(HVDX_KERNEL_LOGPROBS_GRAD, dtype, rows * vocab, st, [&] { return hvdx::launch_logprobs_grad(g, dtype, st); }),
@@ -185,8 +185,9 @@ int hvdx_token_logprobs_grad(const void* logits, int64_t stride, int dtype, int6
 }
 
 size_t hvdx_distill_workspace_bytes(int64_t rows, int64_t vocab) {
-  (void)rows, (void)vocab;
-  return 0;
+  if (rows < 1 || rows > kMostRows || vocab < 1 || vocab > HVDX_MAX_VOCAB) return 0;
+  const int parts = hvdx::row_parts(rows, vocab);
+  return parts == 1 ? 0 : (size_t)rows * parts * 16;
 }
 
 int hvdx_distill(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
@@ -197,7 +198,7 @@ int hvdx_distill(const void* logits, int64_t stride, int dtype, int64_t rows, in
   if (grad)
     if (int rc = check_stride("grad", grad_stride, vocab, rows, what)) return rc;
   if (rows == 0) return HVDX_OK;
-  if (!logits) return fail(HVDX_ERR_INVALID, "%s: logits is NULL", what);
+  if (!logits || !stats) return fail(HVDX_ERR_INVALID, "%s: logits or stats is NULL", what);
   if (grad && !grad_loss) return fail(HVDX_ERR_INVALID, "%s: grad needs grad_loss", what);
   const size_t need = hvdx_distill_workspace_bytes(rows, vocab);
   if (int rc = check_workspace(workspace, workspace_bytes, need, what)) return rc;
@@ -205,14 +206,23 @@ int hvdx_distill(const void* logits, int64_t stride, int dtype, int64_t rows, in
   const Buffer in[] = {matrix("logits", logits, rows, vocab, stride, es), vec("ids", ids, rows * entries, 8),
                        vec("teacher", teacher, rows * entries, 4), vec("grad_loss", grad_loss, rows, 4)};
   const Buffer out[] = {matrix("grad", grad, rows, vocab, grad_stride, es), vec("loss", loss, rows, 4),
-                        vec("stats", stats, rows * 4, 4, 16), vec("workspace", workspace, (int64_t)need, 1)};
+                        vec("stats", stats, rows * 8, 4, 16), vec("workspace", workspace, (int64_t)need, 1)};
   const unsigned same[4] = {1, 0, 0, 0};
   if (int rc = check_buffers(in, 4, out, 4, same, what)) return rc;
-  const hvdx::DistillArgs g{logits, stride, rows, (int)vocab, scale, ids, teacher, entries, rest, grad_loss, loss,
-                            reinterpret_cast<float4*>(stats), grad, grad_stride};
+  hvdx::DistillArgs g{};
+  g.logits = logits, g.stride = stride, g.rows = rows, g.vocab = (int)vocab, g.scale = scale;
+  g.ids = ids, g.teacher = teacher, g.entries = entries, g.rest = rest, g.grad_loss = grad_loss;
+  g.loss = loss, g.stats = reinterpret_cast<hvdx::DistillStats*>(stats), g.grad = grad, g.grad_stride = grad_stride;
+  g.parts = hvdx::distill_parts(rows, vocab, dtype, grad != nullptr);
+  g.part_sums = static_cast<float4*>(workspace);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  TimedLaunch phase(HVDX_KERNEL_DISTILL, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
-  return launched(timed(HVDX_KERNEL_DISTILL, dtype, rows * vocab, st, [&] { return hvdx::launch_distill(g, dtype, st); }), what);
+  const int kind = HVDX_KERNEL_DISTILL, launches = g.parts == 1 ? 1 : grad ? 3 : 2;
+  TimedLaunch phase(kind, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true, launches);
+  hipError_t e = timed(kind, dtype, rows * vocab, st, [&] { return hvdx::launch_distill(g, dtype, st); });
+  if (e == hipSuccess && launches > 1) e = timed(kind, dtype, rows * vocab, st, [&] { return hvdx::launch_distill_join(g, dtype, st); });
+  if (e == hipSuccess && launches > 2)
+    e = timed(HVDX_KERNEL_DISTILL_GRAD, dtype, rows * vocab, st, [&] { return hvdx::launch_distill_grad(g, dtype, st); });
+  return launched(e, what);
 }
 
 int hvdx_distill_grad(const void* logits, int64_t stride, int dtype, int64_t rows, int64_t vocab, float scale,
@@ -227,12 +237,15 @@ int hvdx_distill_grad(const void* logits, int64_t stride, int dtype, int64_t row
   const int es = row_elem_size(dtype);
   const Buffer in[] = {matrix("logits", logits, rows, vocab, stride, es), vec("ids", ids, rows * entries, 8),
                        vec("teacher", teacher, rows * entries, 4), vec("grad_loss", grad_loss, rows, 4),
-                       vec("stats", stats, rows * 4, 4, 16)};
+                       vec("stats", stats, rows * 8, 4, 16)};
   const Buffer out[] = {matrix("grad", grad, rows, vocab, grad_stride, es)};
   const unsigned same[1] = {1};
   if (int rc = check_buffers(in, 5, out, 1, same, what)) return rc;
-  const hvdx::DistillArgs g{logits, stride, rows, (int)vocab, scale, ids, teacher, entries, rest, grad_loss, nullptr,
-                            const_cast<float4*>(reinterpret_cast<const float4*>(stats)), grad, grad_stride};
+  hvdx::DistillArgs g{};
+  g.logits = logits, g.stride = stride, g.rows = rows, g.vocab = (int)vocab, g.scale = scale;
+  g.ids = ids, g.teacher = teacher, g.entries = entries, g.rest = rest, g.grad_loss = grad_loss;
+  g.stats = const_cast<hvdx::DistillStats*>(reinterpret_cast<const hvdx::DistillStats*>(stats));
+  g.grad = grad, g.grad_stride = grad_stride;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   TimedLaunch phase(HVDX_KERNEL_DISTILL_GRAD, -1, 0, dtype, HVDX_COMPRESS_NONE, rows * vocab, st, -1, true);
   return launched(timed(HVDX_KERNEL_DISTILL_GRAD, dtype, rows * vocab, st, [&] { return hvdx::launch_distill_grad(g, dtype, st); }),

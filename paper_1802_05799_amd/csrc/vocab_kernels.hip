@@ -3,11 +3,12 @@
 //
 // For a row z with scale s (one over the temperature): d_v = s (z_v - m) with m the row's
 // largest logit, S = sum e^{d_v}, L = log S, so that log p_v = d_v - L, and the entropy is
-// L - (sum e^{d_v} d_v) / S.  One pass gives all of it: m, S and the weighted sum are carried
-// along, rescaled where the maximum grows.  Exponents are to base 2 (d times log2 e) for the
-// hardware's exponential; z - m is formed before it is scaled, so logits near a type's lowest
-// value (masks) do not overflow.  Everything is held in binary32.  Bound: memory, one read of
-// the logits, and a gradient's one write.
+// L - (sum e^{d_v} d_v) / S.  One pass gives all of it: a reference near the maximum, S and the weighted sum
+// are carried along, rescaled where the reference rises.  Everything is held in binary32.  Bound: memory, one
+// read of the logits and a gradient's one write; 16-bit logits leave some 15 vector operations an element at
+// that rate, of which the exponential takes four.
+#include <type_traits>
+
 #include "rows.hpp"
 
 namespace hvdx {
@@ -18,8 +19,9 @@ namespace {
 constexpr int64_t kBlocksWanted = 1024, kPartLeast = 4096;
 constexpr int kPartsMost = 64;  // one lane each when they are joined
 
-constexpr float kNone = -3.402823466e38f;  // the maximum of nothing: finite, so that -inf minus it is no NaN
+constexpr float kNone = -3.402823466e38f;  // the reference of nothing: finite, so that -inf minus it is no NaN
 constexpr float kFar = -1000.f;            // 2^kFar is 0; a clamp for what 0 is multiplied by
+constexpr float kPlain = 1e30f;            // beyond it a scaled logit might overflow
 
 // A row's elements in 16-byte vectors on 16-byte boundaries, and the few before and after them.
 template <typename T>
@@ -33,52 +35,111 @@ struct Cut {
     edges = vocab - nvec * n;
   }
   __device__ int start(int vec) const { return head + vec * n; }
+  __device__ const Packed<T>* of(const T* row, int first) const {
+    return reinterpret_cast<const Packed<T>*>(row + head) + first;
+  }
+  __device__ T* of(T* row, int first) const { return row + head + first * n + threadIdx.x * n; }
   __device__ int edge(int i) const { return i < head ? i : nvec * n + i; }  // 0 <= i < edges
 };
 
-// max, sum of 2^(d - max) and the sum of those times their exponent, for a part of a row
-struct Online {
-  float m = kNone, s = 0.f, a = 0.f;
-  __device__ void rise(float to, float c) {  // to >= m
-    const float d = fmaxf((m - to) * c, kFar), r = exp2_hw(d);
-    a = r * (a + d * s);
-    s *= r;
-    m = to;
-  }
-  __device__ void add(float z, float c) {
-    const float d = (z - m) * c, e = exp2_hw(d);
-    s += e;
-    a += e * fmaxf(d, kFar);
-  }
-  __device__ void join(Online o, float c) {
-    const float hi = fmaxf(m, o.m);
-    rise(hi, c);
-    o.rise(hi, c);
-    s += o.s;
-    a += o.a;
+// Exponents to base 2 (for the hardware's exponential) of logits against a reference.  Ordinarily the reference is
+// the scaled maximum, c z_max with c = s log2 e, and an exponent c z - ref is one fused operation.  WIDE: the
+// reference is the maximum itself and the difference is taken first, for rows whose scaled maximum is
+// beyond kPlain (a row masked throughout with a type's lowest value is still uniform).
+template <bool WIDE>
+struct Scale {
+  float c;
+  static constexpr float nothing = WIDE ? kNone : -kPlain;
+  __device__ float reference(float z) const { return WIDE ? z : z * c; }
+  __device__ float exponent(float z, float ref) const { return WIDE ? (z - ref) * c : fmaf(z, c, -ref); }
+  __device__ float between(float low, float high) const { return fmaxf(WIDE ? (low - high) * c : low - high, kFar); }
+  // weight times the exponent to base e; finite for a logit of a type's lowest value
+  __device__ float natural(float z, float ref, float scale, float weight) const {
+    if (WIDE) return weight * scale * (z - ref);
+    const float d = exponent(z, ref);
+    return d == -__builtin_inff() && z > d ? weight * scale * z : weight * (kLn2 * d);
   }
 };
+__device__ __forceinline__ bool plain(float ref) { return ref > -kPlain && ref < kPlain; }
 
-template <int W>
-__device__ Online block_join(Online o, float c, float (*lds)[3]) {  // the same in every thread
-#pragma unroll
-  for (int k = 1; k < 64; k *= 2) {
-    Online other;
-    other.m = __shfl_xor(o.m, k);
-    other.s = __shfl_xor(o.s, k);
-    other.a = __shfl_xor(o.a, k);
-    o.join(other, c);
+// Reference, sum of 2^exponent, and the sum of those times their exponent, of a part of a row.
+template <bool WIDE>
+struct Sums {
+  float ref = Scale<WIDE>::nothing, s = 0.f, a = 0.f;
+  __device__ void rise(float to, Scale<WIDE> k) {
+    const float d = k.between(ref, to), r = exp2_hw(d);
+    a = r * (a + d * s);
+    s *= r;
+    ref = to;
   }
+  template <bool ENTROPY>
+  __device__ void add(float z, Scale<WIDE> k) {
+    const float d = k.exponent(z, ref), e = exp2_hw(d);
+    s += e;
+    if constexpr (ENTROPY) a = fmaf(e, fmaxf(d, kFar), a);
+  }
+  template <bool ENTROPY>
+  __device__ void one(float z, Scale<WIDE> k) {
+    const float r = k.reference(z);
+    if (r > ref) rise(r, k);
+    add<ENTROPY>(z, k);
+  }
+  __device__ void over_lanes(Scale<WIDE> k) {
+    rise(wave_max(ref), k);
+    s = wave_sum(s);
+    a = wave_sum(a);
+  }
+};
+template <int W, bool WIDE>
+__device__ __forceinline__ Sums<WIDE> over_block(Sums<WIDE> o, Scale<WIDE> k, float (*lds)[3]) {  // in every thread
+  o.over_lanes(k);
   if constexpr (W > 1) {
-    if (threadIdx.x % 64 == 0) {
+    const int lane = threadIdx.x % 64;
+    __syncthreads();  // of what read it before
+    if (lane == 0) {
       float* mine = lds[threadIdx.x / 64];
-      mine[0] = o.m, mine[1] = o.s, mine[2] = o.a;
+      mine[0] = o.ref, mine[1] = o.s, mine[2] = o.a;
     }
     __syncthreads();
-    o = Online{lds[0][0], lds[0][1], lds[0][2]};
-    for (int w = 1; w < W; ++w) o.join(Online{lds[w][0], lds[w][1], lds[w][2]}, c);
+    o = Sums<WIDE>{};
+    if (lane < W) o = Sums<WIDE>{lds[lane][0], lds[lane][1], lds[lane][2]};
+    o.over_lanes(k);
   }
   return o;
+}
+
+template <typename T>
+__device__ __forceinline__ float largest(Wide<T> x) {
+  float h = x[0];
+#pragma unroll
+  for (int k = 1; k < RowTypes<T>::n; ++k) h = fmaxf(h, x[k]);
+  return h;
+}
+
+// kBatch vectors are loaded at once, and the sums rescaled once for each batch.
+constexpr int kBatch = 4;
+template <bool ENTROPY, bool WIDE, typename T, int B>
+__device__ __forceinline__ void add_batch(Sums<WIDE>& o, Scale<WIDE> k, const Wide<T> (&x)[B], float high) {
+  const float r = k.reference(high);
+  if (r > o.ref) o.rise(r, k);
+#pragma unroll
+  for (int u = 0; u < B; ++u)
+#pragma unroll
+    for (int e = 0; e < RowTypes<T>::n; ++e) o.template add<ENTROPY>(x[u][e], k);
+}
+// each(first, p) for the thread's vectors in [v0, v1), kBatch at a time.
+template <int NT, bool STREAM, typename T, typename Each>
+__device__ __forceinline__ void for_batches(const T* z, const Cut<T>& cut, int v0, int v1, Each each) {
+  for (int i = v0 + (int)threadIdx.x; i < v1; i += kBatch * NT) {
+    Packed<T> p[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (i + u * NT < v1) {
+        const auto* at = reinterpret_cast<const Packed<T>*>(z + cut.start(i + u * NT));
+        p[u] = STREAM ? __builtin_nontemporal_load(at) : *at;
+      }
+    each(i, p);
+  }
 }
 
 // An order of (value, position): larger values first, then lower positions; -0 as +0.
@@ -168,165 +229,203 @@ __device__ void select_top(int k, uint64_t best, TopLds<W>& lds, Collect collect
   }
 }
 
-// What a row's sums give, and one of its alternatives.
-__device__ __forceinline__ void finish_logprobs(const LogprobArgs& g, int64_t row, float z_token, int64_t token, Online o) {
-  const bool none = o.s == 0.f;
-  const float lse = logf(o.s), entropy = none ? 0.f : lse - kLn2 * o.a / o.s;
-  if (g.logprob) {
-    float lp = 0.f;
-    if (token >= g.vocab) lp = __builtin_nanf("");
-    else if (token >= 0) lp = none ? -__builtin_inff() : (z_token - o.m) * g.scale - lse;
-    g.logprob[row] = lp;
+// A row's sums as its results take them: log2 of the sum beside the reference, or what there is none for.
+struct RowSums {
+  float ref, log2s, entropy;
+  bool wide, none, broken;
+  __device__ float log_p(float z, float scale) const {
+    const float c = scale * kLog2e;
+    if (none) return broken ? __builtin_nanf("") : -__builtin_inff();
+    return (wide ? Scale<true>{c}.natural(z, ref, scale, 1.f) : Scale<false>{c}.natural(z, ref, scale, 1.f)) - kLn2 * log2s;
   }
-  if (g.entropy) g.entropy[row] = entropy;
-  if (g.stats) g.stats[row] = make_float4(o.m, lse, entropy, 0.f);
+};
+template <bool WIDE>
+__device__ __forceinline__ RowSums row_sums(Sums<WIDE> o) {
+  RowSums r{o.ref, log2f(o.s), 0.f, WIDE, o.s == 0.f, !(o.s == o.s)};
+  if (!r.none) r.entropy = kLn2 * (r.log2s - o.a / o.s);
+  return r;
 }
-__device__ __forceinline__ void emit_top(const LogprobArgs& g, int64_t row, int rank, uint64_t key, Online o) {
-  const bool broken = !(o.s == o.s);
-  g.top_ids[row * g.top + rank] = broken ? -1 : key_position(key);
-  g.top_logprobs[row * g.top + rank] = broken ? __builtin_nanf("")
-                                       : o.s == 0.f ? -__builtin_inff()
-                                                    : (key_value(key) - o.m) * g.scale - logf(o.s);
+__device__ __forceinline__ void finish_logprobs(const LogprobArgs& g, int64_t row, float z_token, int64_t token, RowSums r) {
+  if (g.logprob) g.logprob[row] = token >= g.vocab ? __builtin_nanf("") : token < 0 ? 0.f : r.log_p(z_token, g.scale);
+  if (g.entropy) g.entropy[row] = r.entropy;
+  if (g.stats) g.stats[row] = make_float4(r.ref, r.log2s, r.entropy, r.wide ? 1.f : 0.f);
+}
+__device__ __forceinline__ void emit_top(const LogprobArgs& g, int64_t row, int rank, uint64_t key, RowSums r) {
+  g.top_ids[row * g.top + rank] = r.broken ? -1 : key_position(key);
+  g.top_logprobs[row * g.top + rank] = r.broken ? __builtin_nanf("") : r.log_p(key_value(key), g.scale);
 }
 
 // A block has one of a row's `parts`: all of it, and the results, or a stretch of its vectors, whose sums and
-// first keys go to the workspace for logprobs_join_kernel.  kBatch vectors are loaded at once, and
-// the sums rescaled once for each batch.
-constexpr int kBatch = 4;
-template <typename T, int W>
+// first keys go to the workspace for logprobs_join_kernel.
+//
+// For the alternatives a thread notes the largest of its elements, and in LDS the largest of each of kNotes
+// stretches of its vectors: of the stretches that reach the bound it reads its own again, and no
+// others.  (Reading all its vectors again, 16 bytes of each line, cost as much as the pass itself.)
+constexpr int kNotes = 16;
+template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
   constexpr int NT = 64 * W, N = RowTypes<T>::n;
   __shared__ float parts[W][3];
-  __shared__ TopLds<W> top;
+  __shared__ TopLds<TOP ? W : 1> top;
+  __shared__ float notes[TOP ? kNotes : 1][TOP ? NT : 1];
   const int64_t block = block_row();
   if (block >= g.rows * g.parts) return;
   const int64_t row = g.parts == 1 ? block : block / g.parts;
   const int part = g.parts == 1 ? 0 : (int)(block % g.parts);
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
-  const float c = g.scale * kLog2e;
+  const Scale<false> k{g.scale * kLog2e};
   const Cut<T> cut(z, g.vocab);
   const int v0 = (int)((int64_t)cut.nvec * part / g.parts), v1 = (int)((int64_t)cut.nvec * (part + 1) / g.parts);
   const int edges = part == 0 ? cut.edges : 0;
+  const bool has_edge = (int)threadIdx.x < edges;
+  const int edge_at = has_edge ? cut.edge(threadIdx.x) : -1;
+  const float edge = has_edge ? (float)z[edge_at] : -__builtin_inff();
   const int64_t token = g.logprob ? g.tokens[row] : -1;
   const float z_token = token >= 0 && token < g.vocab ? (float)z[token] : 0.f;
-  Online o;
+  Sums<false> o;
   float high = -__builtin_inff();  // the thread's largest, and where its vector (or edge element) starts
-  int high_at = v0 + (int)threadIdx.x < v1 ? cut.start(v0 + threadIdx.x) : (int)threadIdx.x < edges ? cut.edge(threadIdx.x) : -1;
-  for (int i = v0 + threadIdx.x; i < v1; i += kBatch * NT) {
-    Packed<T> p[kBatch];
-    bool there[kBatch];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      there[u] = i + u * NT < v1;
-      if (there[u]) p[u] = load_packed(z + cut.start(i + u * NT));
-    }
+  int high_at = v0 + (int)threadIdx.x < v1 ? cut.start(v0 + threadIdx.x) : edge_at;
+  const int batches = (v1 - v0 + kBatch * NT - 1) / (kBatch * NT), per_note = (batches + kNotes - 1) / kNotes;
+  int note = 0, left = per_note;
+  float noted = -__builtin_inff();
+  for_batches<NT, !TOP>(z, cut, v0, v1, [&](int i, const Packed<T>(&p)[kBatch]) {
     Wide<T> x[kBatch];
     float hi = kNone;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      x[u] = there[u] ? widen<T>(p[u]) : Wide<T>(-__builtin_inff());
-      float h = x[u][0];
-#pragma unroll
-      for (int k = 1; k < N; ++k) h = fmaxf(h, x[u][k]);
-      if (h > high) {
+      x[u] = i + u * NT < v1 ? widen<T>(p[u]) : Wide<T>(-__builtin_inff());
+      const float h = largest<T>(x[u]);
+      if (TOP && h > high) {
         high = h;
         high_at = cut.start(i + u * NT);
       }
       hi = fmaxf(hi, h);
     }
-    if (hi > o.m) o.rise(hi, c);
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-#pragma unroll
-      for (int k = 0; k < N; ++k) o.add(x[u][k], c);
-  }
-  if ((int)threadIdx.x < edges) {
-    const float x = (float)z[cut.edge(threadIdx.x)];
-    if (high_at < 0 || key_of(x, cut.edge(threadIdx.x)) > key_of(high, high_at)) {  // it may stand before the vectors
-      high = x;
-      high_at = cut.edge(threadIdx.x);
+    add_batch<true, false, T>(o, k, x, hi);
+    if constexpr (TOP) {
+      noted = fmaxf(noted, hi);
+      notes[note][threadIdx.x] = noted;
+      if (--left == 0) {
+        left = per_note;
+        noted = -__builtin_inff();
+        ++note;
+      }
     }
-    if (x > o.m) o.rise(x, c);
-    o.add(x, c);
+  });
+  if (has_edge) {
+    o.one<true>(edge, k);
+    if (TOP && (high_at < 0 || key_of(edge, edge_at) > key_of(high, high_at))) {  // it may stand before the vectors
+      high = edge;
+      high_at = edge_at;
+    }
   }
-  o = block_join<W>(o, c, parts);
+  o = over_block<W>(o, k, parts);
+  RowSums r;
+  float4 sums = make_float4(o.ref, o.s, o.a, 0.f);
+  if (plain(o.ref)) {
+    r = row_sums(o);
+  } else {
+    const Scale<true> kw{k.c};
+    Sums<true> w;
+    for (int i = v0 + threadIdx.x; i < v1; i += NT) {
+      const Wide<T> x[1] = {widen<T>(load_packed(z + cut.start(i)))};
+      add_batch<true, true, T>(w, kw, x, largest<T>(x[0]));
+    }
+    if (has_edge) w.one<true>(edge, kw);
+    w = over_block<W>(w, kw, parts);
+    r = row_sums(w);
+    sums = make_float4(w.ref, w.s, w.a, 1.f);
+  }
   const bool whole = g.parts == 1;
   if (threadIdx.x == 0) {
-    if (whole) finish_logprobs(g, row, z_token, token, o);
-    else g.part_sums[block] = make_float4(o.m, o.s, o.a, 0.f);
+    if (whole) finish_logprobs(g, row, z_token, token, r);
+    else g.part_sums[block] = sums;
   }
-  if (!g.top) return;
-  select_top<W>(
-      g.top, high_at < 0 ? 0 : key_of(high, high_at), top,
-      [&](uint64_t bound, auto push) {
-        for (int i = v0 + threadIdx.x; i < v1; i += kBatch * NT) {
-          Packed<T> p[kBatch];
+  if constexpr (TOP) {
+    select_top<W>(
+        g.top, high_at < 0 ? 0 : key_of(high, high_at), top,
+        [&](uint64_t bound, auto push) {
+          const float least = key_value(bound);
+          int n = 0;
+          for (int b = 0; b < batches; ++n) {
+            const int end = b + per_note < batches ? b + per_note : batches;
+            if (bound && v0 + (int)threadIdx.x + b * kBatch * NT < v1 && notes[n][threadIdx.x] < least) {
+              b = end;
+              continue;
+            }
+            for (int i = v0 + threadIdx.x + b * kBatch * NT; i < v1 && i < v0 + end * kBatch * NT; i += NT) {
+              const int start = cut.start(i);
+              const Wide<T> x = widen<T>(load_packed(z + start));
+              if (key_of(largest<T>(x), start) < bound) continue;
 #pragma unroll
-          for (int u = 0; u < kBatch; ++u)
-            if (i + u * NT < v1) p[u] = load_packed(z + cut.start(i + u * NT));
-#pragma unroll
-          for (int u = 0; u < kBatch; ++u) {
-            if (i + u * NT >= v1) break;
-            const int start = cut.start(i + u * NT);
-            const Wide<T> x = widen<T>(p[u]);
-            float h = x[0];
-#pragma unroll
-            for (int k = 1; k < N; ++k) h = fmaxf(h, x[k]);
-            if (key_of(h, start) < bound) continue;
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-              if (key_of(x[k], start) >= bound) push(key_of(x[k], start + k));
+              for (int e = 0; e < N; ++e)
+                if (key_of(x[e], start) >= bound) push(key_of(x[e], start + e));
+            }
+            b = end;
           }
-        }
-        if ((int)threadIdx.x < edges) {
-          const uint64_t key = key_of((float)z[cut.edge(threadIdx.x)], cut.edge(threadIdx.x));
-          if (key >= bound) push(key);
-        }
-      },
-      [&](uint64_t last) {
-        uint64_t next = 0;
-        auto take = [&](float x, int at) {
-          const uint64_t key = key_of(x, at);
-          if (key < last && key > next) next = key;
-        };
-        for (int i = v0 + threadIdx.x; i < v1; i += NT) {
-          const Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
+          if (has_edge && key_of(edge, edge_at) >= bound) push(key_of(edge, edge_at));
+        },
+        [&](uint64_t last) {
+          uint64_t next = 0;
+          auto take = [&](float x, int at) {
+            const uint64_t key = key_of(x, at);
+            if (key < last && key > next) next = key;
+          };
+          for (int i = v0 + threadIdx.x; i < v1; i += NT) {
+            const Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
 #pragma unroll
-          for (int k = 0; k < N; ++k) take(x[k], cut.start(i) + k);
-        }
-        if ((int)threadIdx.x < edges) take((float)z[cut.edge(threadIdx.x)], cut.edge(threadIdx.x));
-        return next;
-      },
-      [&](int rank, uint64_t key) {
-        if (whole) emit_top(g, row, rank, key, o);
-        else g.part_keys[block * g.top + rank] = key;
-      });
+            for (int e = 0; e < N; ++e) take(x[e], cut.start(i) + e);
+          }
+          if (has_edge) take(edge, edge_at);
+          return next;
+        },
+        [&](int rank, uint64_t key) {
+          if (whole) emit_top(g, row, rank, key, r);
+          else g.part_keys[block * g.top + rank] = key;
+        });
+  }
 }
 
-// A row's results from its parts'.
-template <typename T>
-__global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs g) {
+// One lane's part joined with the others'.  Among parts a row is WIDE where one with any weight (or a listed
+// token, `huge`) has an enormous logit, or none is ordinary; the ordinary parts' references are then unscaled.
+__device__ __forceinline__ bool wide_row(bool there, float4 sums, bool huge) {
+  const bool weight = there && !(sums.y == 0.f);
+  const bool high = __any(huge || (weight && sums.w != 0.f && sums.x > 0.f)), ordinary = __any(weight && sums.w == 0.f);
+  return high || !ordinary;
+}
+template <bool WIDE>
+__device__ __forceinline__ Sums<WIDE> join_parts(bool there, float4 sums, Scale<WIDE> k) {
+  Sums<WIDE> o;
+  if (there && (WIDE || sums.w == 0.f)) o = Sums<WIDE>{WIDE && sums.w == 0.f ? sums.x / k.c : sums.x, sums.y, sums.z};
+  o.over_lanes(k);
+  return o;
+}
+
+// A row's results from its parts': every wavefront joins the sums, the block selects among the keys.
+__global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs g, int dtype) {
   constexpr int NT = 64 * kWaves;
-  __shared__ float parts[kWaves][3];
   __shared__ TopLds<kWaves> top;
   const int64_t row = block_row();
   if (row >= g.rows) return;
-  const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   const float c = g.scale * kLog2e;
   const int64_t token = g.logprob ? g.tokens[row] : -1;
-  const float z_token = token >= 0 && token < g.vocab ? (float)z[token] : 0.f;
-  const uint64_t* keys = g.part_keys + row * g.parts * g.top;
-  const int nkeys = g.parts * g.top;
-  Online o;
-  if ((int)threadIdx.x < g.parts) {
-    const float4 s = g.part_sums[row * g.parts + threadIdx.x];
-    o = Online{s.x, s.y, s.z};
+  float z_token = 0.f;
+  if (token >= 0 && token < g.vocab) {
+    const int64_t at = row * g.stride + token;
+    z_token = dtype == HVDX_FLOAT32   ? static_cast<const float*>(g.logits)[at]
+              : dtype == HVDX_FLOAT16 ? (float)static_cast<const _Float16*>(g.logits)[at]
+                                      : (float)static_cast<const __bf16*>(g.logits)[at];
   }
+  const uint64_t* keys = g.part_keys + row * g.parts * g.top;
+  const int nkeys = g.parts * g.top, lane = threadIdx.x % 64;
+  const bool there = lane < g.parts;
+  const float4 sums = there ? g.part_sums[row * g.parts + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
   uint64_t best = 0;
   for (int i = threadIdx.x; i < nkeys; i += NT)
     if (keys[i] > best) best = keys[i];
-  o = block_join<kWaves>(o, c, parts);
-  if (threadIdx.x == 0) finish_logprobs(g, row, z_token, token, o);
+  const RowSums r = wide_row(there, sums, false) ? row_sums(join_parts<true>(there, sums, Scale<true>{c}))
+                                                : row_sums(join_parts<false>(there, sums, Scale<false>{c}));
+  if (threadIdx.x == 0) finish_logprobs(g, row, z_token, token, r);
   if (!g.top) return;
   select_top<kWaves>(
       g.top, best, top,
@@ -340,107 +439,94 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs 
           if (keys[i] < last && keys[i] > next) next = keys[i];
         return next;
       },
-      [&](int rank, uint64_t key) { emit_top(g, row, rank, key, o); });
+      [&](int rank, uint64_t key) { emit_top(g, row, rank, key, r); });
 }
 
-// dz_v = s [ a (delta - p_v) - b p_v (log p_v + H) ] = p_v (C0 + C1 d_v) + s a delta, d_v in base 2.
+// The gradients are element by element: a block has kChunk vectors of a row.
+constexpr int kChunkBatches = 2, kChunk = kChunkBatches * kBatch * 64 * kWaves;
+inline int64_t row_chunks(int64_t vocab, int n) {
+  const int64_t chunks = (vocab / n + kChunk - 1) / kChunk;
+  return chunks < 1 ? 1 : chunks;
+}
+// out = f(z, position) over a block's chunk of a row; the first chunk has the edges too.
+template <typename T, typename F>
+__device__ __forceinline__ void map_chunk(const T* z, T* out, const Cut<T>& cut, int chunk, F f) {
+  constexpr int NT = 64 * kWaves, N = RowTypes<T>::n;
+  const int v0 = chunk * kChunk, v1 = v0 + kChunk < cut.nvec ? v0 + kChunk : cut.nvec;
+  for_batches<NT, true>(z, cut, v0, v1, [&](int i, const Packed<T>(&p)[kBatch]) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (i + u * NT >= v1) break;
+      const int start = cut.start(i + u * NT);
+      Wide<T> x = widen<T>(p[u]);
+#pragma unroll
+      for (int e = 0; e < N; ++e) x[e] = f(x[e], start + e);
+      store_packed(out + start, narrow<T>(x));
+    }
+  });
+  if (chunk == 0 && (int)threadIdx.x < cut.edges) {
+    const int at = cut.edge(threadIdx.x);
+    out[at] = (T)f((float)z[at], at);
+  }
+}
+
+// dz_v = s [ a (delta - p_v) - b p_v (log p_v + H) ] = 2^{d_v} (C0 + C1 d_v) + s a delta, d_v to base 2.
 template <typename T>
 __global__ __launch_bounds__(64 * kWaves) void logprobs_grad_kernel(LogprobGradArgs g) {
-  constexpr int NT = 64 * kWaves, N = RowTypes<T>::n;
-  const int64_t row = block_row();
-  if (row >= g.rows) return;
+  const int64_t block = block_row();
+  if (block >= g.rows * g.chunks) return;
+  const int64_t row = g.chunks == 1 ? block : block / g.chunks;
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
   const float c = g.scale * kLog2e;
   const Cut<T> cut(z, g.vocab);
   const float4 st = g.stats[row];
-  const float m = st.x, lse = st.y, entropy = st.z;
+  const float ref = st.x, log2s = st.y, entropy = st.z;
   const int64_t t = g.tokens ? g.tokens[row] : -1;
   float a = g.grad_logprob && t >= 0 ? g.grad_logprob[row] : 0.f;
   if (g.grad_logprob && t >= g.vocab) a = __builtin_nanf("");
   const float b = g.grad_entropy ? g.grad_entropy[row] : 0.f;
-  const bool none = lse == -__builtin_inff();
-  const float inv = none ? 0.f : expf(-lse);
+  const bool none = log2s == -__builtin_inff();
   if (none) a = 0.f;
-  const float c1 = -g.scale * b * kLn2, c0 = -g.scale * (a + b * (none ? 0.f : entropy - lse));
+  const float over = none ? 0.f : -g.scale * exp2f(-log2s);
+  const float c1 = over * b * kLn2, c0 = over * (a + b * (none ? 0.f : entropy - kLn2 * log2s));
   const float peak = g.scale * a;
-  auto one = [&](float x, int at) {
-    const float d = (x - m) * c;
-    float v = exp2_hw(d) * inv * (c0 + c1 * fmaxf(d, kFar));
-    return at == t ? v + peak : v;
+  const int token = t >= 0 && t < g.vocab ? (int)t : -1;
+  auto run = [&](auto k) {
+    map_chunk(z, out, cut, (int)(block - row * g.chunks), [&](float x, int at) {
+      const float d = k.exponent(x, ref);
+      const float v = exp2_hw(d) * fmaf(c1, fmaxf(d, kFar), c0);
+      return at == token ? v + peak : v;
+    });
   };
-  for (int i = threadIdx.x; i < cut.nvec; i += NT) {
-    Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
-#pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = one(x[k], cut.start(i) + k);
-    store_packed(out + cut.start(i), narrow<T>(x));
-  }
-  if ((int)threadIdx.x < cut.edges) {
-    const int at = cut.edge(threadIdx.x);
-    out[at] = (T)one((float)z[at], at);
-  }
+  if (st.w == 0.f) run(Scale<false>{c});
+  else run(Scale<true>{c});
 }
 
 // What the teacher's alternatives ask of a row, in lane j of one wavefront for entry j.
 struct Entry {
-  int64_t id;     // -1 where absent
+  int id;         // -1 where absent
   float z, q;     // the student's logit there, the teacher's probability
   float log_q;
   bool first;     // of the entries with this token
   float q_token;  // the probability of all of them
 };
 
-constexpr int kBitmapMost = 32768;  // bytes: one for each vector of a row, by its number modulo their count
-
-// Distillation.  `rest`: what is left of the teacher's mass, q_R, stands against the unlisted tokens'
-// p_R, whose sum is taken over them alone (subtracting the listed ones' from the whole would lose
-// it where they hold nearly everything): the pass leaves the listed tokens out, which a bitmap in LDS
-// marks, and the wavefront that holds the entries adds theirs afterwards.  An unlisted token's
-// gradient is then s g 2^(d) F with d from the unlisted maximum m_R and
-// F = Q 2^(m_R - m) / S - q_R / S_R; a listed one's is s g (Q p - q), written over it.
-template <typename T, bool REST>
-struct DistillRow {
-  static constexpr int N = RowTypes<T>::n;
-  const T* z;
-  Cut<T> cut;
-  int vocab, entries;
-  uint32_t mask;
-  bool exact;
-  const uint8_t* bitmap;
-  const int* listed;  // LDS [64], -1 for absent entries
-
-  __device__ uint32_t marks(int vec) const {
-    uint32_t b = bitmap[vec & mask];
-    if (b && !exact) {
-      b = 0;
-      for (int j = 0; j < entries; ++j) {
-        const int d = listed[j] - cut.start(vec);
-        if (listed[j] >= 0 && d >= 0 && d < N) b |= 1u << d;
-      }
-    }
-    return b;
-  }
-  __device__ bool is_listed(int at) const {
-    for (int j = 0; j < entries; ++j)
-      if (listed[j] == at) return true;
-    return false;
-  }
-};
-
 template <typename T, bool REST>
 __device__ __forceinline__ Entry entry_of(const DistillArgs& g, const T* z, int64_t row, int lane, bool& bad) {
   Entry e{-1, 0.f, 0.f, 0.f, true, 0.f};
   float t = -__builtin_inff();
+  bool outside = false;
   if (lane < g.entries) {
-    e.id = g.ids[row * g.entries + lane];
-    if (e.id >= g.vocab) bad = true;
-    if (e.id < 0 || e.id >= g.vocab) e.id = -1;
-    if (e.id >= 0) {
+    const int64_t id = g.ids[row * g.entries + lane];
+    outside = id >= g.vocab;
+    if (id >= 0 && !outside) {
+      e.id = (int)id;
       t = g.teacher[row * g.entries + lane];
-      e.z = (float)z[e.id];
+      e.z = (float)z[id];
     }
   }
-  bad = __any(bad);
+  bad = __any(outside);
   if constexpr (!REST) {
     const float high = wave_max(t);
     const float x = high == -__builtin_inff() ? t : t - high;
@@ -449,11 +535,10 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& g, const T* z, int6
   }
   e.q = e.id >= 0 ? expf(t) : 0.f;
   e.log_q = t;
-  e.q_token = 0.f;
   for (int j = 0; j < g.entries; ++j) {
-    const int id = __shfl((int)e.id, j);
-    const float q = __shfl(e.q, j);
-    if (id == (int)e.id) {
+    const int id = __builtin_amdgcn_readlane(e.id, j);
+    const float q = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e.q), j));
+    if (id == e.id) {
       e.q_token += q;
       if (j < lane) e.first = false;
     }
@@ -461,176 +546,375 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& g, const T* z, int6
   return e;
 }
 
-// The row's loss and what its gradient takes, from the pass over the unlisted (REST) or all tokens.
-struct DistillResult {
-  float loss, f, m, lse, total;
+// With `rest`, what is left of the teacher's mass, q_R, stands against the unlisted tokens' p_R, whose sum is taken
+// over them alone (subtracting the listed ones' from the whole would lose it where they hold nearly
+// everything): the pass leaves the listed tokens out, which a bitmap in LDS marks, a byte for each
+// vector (of a long row: by its number modulo the bitmap's bytes, a mark then being looked up among the
+// entries), and the wavefront that holds the entries adds theirs afterwards.  An unlisted token's gradient is
+// s g 2^d F with d against the unlisted tokens' reference R and F = Q 2^{R - r} / S - q_R / S_R, r and S
+// the row's; a listed one's is s g (Q p - q), written over it.
+constexpr uint32_t kBitmapMost = 16384;  // as many as a row in registers has vectors
+constexpr int64_t kRowMost = 16384;
+struct Listed {
+  const uint8_t* bitmap;
+  uint32_t mask;
+  const int* ids;  // LDS, -1 for absent entries
+  int entries;
+  template <int N>
+  __device__ uint32_t marks(int vec, int start, bool exact) const {
+    uint32_t b = bitmap[vec & mask];
+    if (b && !exact) {
+      b = 0;
+      for (int j = 0; j < entries; ++j)
+        if (ids[j] >= start && ids[j] < start + N) b |= 1u << (ids[j] - start);
+    }
+    return b;
+  }
+  __device__ bool has(int at) const {
+    for (int j = 0; j < entries; ++j)
+      if (ids[j] == at) return true;
+    return false;
+  }
 };
-template <bool REST>
-__device__ __forceinline__ DistillResult distill_finish(const Entry& e, Online o, float scale, bool bad) {
-  const float c = scale * kLog2e, inf = __builtin_inff();
+// The block's bitmap of a row's entries; `ids` [65] and the words are LDS, ids[64] says whether one is `huge`.
+// Ends with a barrier.
+template <int NT, typename T>
+__device__ __forceinline__ Listed list_entries(uint32_t* words, uint32_t mask, int* ids, const Cut<T>& cut, const Entry& e,
+                                               int entries, bool huge) {
+  constexpr int N = RowTypes<T>::n;
+  for (uint32_t i = threadIdx.x; i <= mask / 4; i += NT) words[i] = 0;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    ids[threadIdx.x] = e.id;
+    if (threadIdx.x == 0) ids[64] = huge;
+    const int d = e.id - cut.head;
+    if (e.id >= 0 && d >= 0 && d / N < cut.nvec) {
+      const uint32_t at = (uint32_t)(d / N) & mask;
+      atomicOr(&words[at / 4], 1u << (at % 4 * 8 + d % N));
+    }
+  }
+  __syncthreads();
+  return Listed{reinterpret_cast<const uint8_t*>(words), mask, ids, entries};
+}
+template <typename T>
+__device__ __forceinline__ void leave_out(Wide<T>& x, uint32_t marks) {
+  if (__ballot(marks != 0)) {  // a branch of the wavefront's: few vectors have any
+#pragma unroll
+    for (int e = 0; e < RowTypes<T>::n; ++e)
+      if (marks >> e & 1) x[e] = -__builtin_inff();
+  }
+}
+
+// Whether a listed token's logit makes its row WIDE, though the unlisted ones' would not.
+__device__ __forceinline__ bool huge_entry(const Entry& e, float c) { return e.id >= 0 && !(e.z * c < kPlain); }
+
+// The row's loss and what its gradient takes, from the pass over the unlisted (REST) or all tokens.
+template <bool REST, bool WIDE>
+__device__ __forceinline__ void distill_finish(const Entry& e, Sums<WIDE> o, Scale<WIDE> k, float scale, bool bad, float& loss,
+                                               DistillStats& st) {
+  const float inf = __builtin_inff();
   const bool there = e.id >= 0;
-  float m = o.m, s = o.s, down = 1.f;
+  float ref = o.ref, s = o.s, down = 1.f;
   if constexpr (REST) {
-    m = fmaxf(m, wave_max(there ? e.z : kNone));
-    down = exp2_hw(fmaxf((o.m - m) * c, kFar));
-    s = o.s * down + wave_sum(there && e.first ? exp2_hw((e.z - m) * c) : 0.f);
+    ref = fmaxf(ref, wave_max(there ? k.reference(e.z) : -inf));
+    down = exp2_hw(k.between(o.ref, ref));
+    s = o.s * down + wave_sum(there && e.first ? exp2_hw(k.exponent(e.z, ref)) : 0.f);
   }
   const float lse = logf(s);
   // q (log q - log p), the scale taken with q: what is left of a mask of the lowest value stays finite
-  const float each = s == 0.f ? inf : e.q * (e.log_q + lse) - (e.q * scale) * (e.z - m);
-  const float part = wave_sum(there && !(e.q == 0.f) ? each : 0.f);
+  const float each = s == 0.f ? inf : e.q * (e.log_q + lse) - k.natural(e.z, ref, scale, e.q);
+  loss = wave_sum(there && !(e.q == 0.f) ? each : 0.f);
   const float listed = wave_sum(e.q);
-  DistillResult r{part, 0.f, m, lse, listed};
-  float over = 0.f;
+  float total = listed, over = 0.f;
   if constexpr (REST) {
     const float left = fmaxf(1.f - listed, 0.f);
-    r.total += left;
+    total += left;
     if (left > 0.f) {
       if (!(o.s == 0.f)) {
-        r.loss += left * (logf(left) - ((o.m - m) * scale + logf(o.s) - lse));
+        const float down_log = WIDE ? (o.ref - ref) * scale : kLn2 * (o.ref - ref);
+        loss += left * (logf(left) - (down_log + logf(o.s) - lse));
         over = left / o.s;
       } else if (left > 1e-6f) {  // less is the rounding of a sum that is 1: nothing is left on either side
-        r.loss += inf;
+        loss += inf;
       }
     }
   }
-  r.f = s == 0.f ? 0.f : r.total * down / s - over;
-  if (bad) r.loss = r.f = r.lse = __builtin_nanf("");
-  return r;
+  st = DistillStats{o.ref, s == 0.f ? 0.f : total * down / s - over, ref, log2f(s), total, WIDE ? 1.f : 0.f, 0.f, 0.f};
+  if (bad) loss = st.f = st.log2s = __builtin_nanf("");
 }
 
 template <typename T>
-__device__ __forceinline__ void patch_listed(const DistillArgs& g, T* out, const Entry& e, float scaled, float total,
-                                             float m, float lse) {
+__device__ __forceinline__ void patch_listed(const DistillArgs& g, T* out, const Entry& e, float scaled, const DistillStats& st) {
   if (e.id < 0 || !e.first) return;
-  const float p = expf((e.z - m) * g.scale - lse);
-  out[e.id] = (T)(lse == -__builtin_inff() ? 0.f : scaled * (total * p - e.q_token));
+  const float c = g.scale * kLog2e;
+  const float d = st.wide != 0.f ? Scale<true>{c}.exponent(e.z, st.ref) : Scale<false>{c}.exponent(e.z, st.ref);
+  const float v = scaled * (st.total * exp2f(d - st.log2s) - e.q_token);
+  out[e.id] = (T)(st.log2s == -__builtin_inff() ? 0.f : v);
 }
 
-// Loss, and with `grad` the gradient too, one block a row: the logits are read once for the sums and
-// once more (from a cache) for the gradient.
-template <typename T, bool REST>
-__global__ __launch_bounds__(64 * kWaves) void distill_kernel(DistillArgs g, uint32_t bitmap_mask) {
-  constexpr int NT = 64 * kWaves, N = RowTypes<T>::n;
-  extern __shared__ uint32_t bitmap[];
-  __shared__ float parts[kWaves][3];
-  __shared__ int listed[64];
-  __shared__ float result[5];
+// Sixteen bytes of a row kept in registers.  forget: the same, as far as the compiler knows others, so that it does
+// not keep what was computed of them (in 32 bits they would be twice the registers).
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void forget(Words& v) { asm volatile("" : "+v"(v)); }
+
+// A block's work on a row or one of its parts: where it is, and what it has in LDS and of the entries.
+template <typename T>
+struct DistillBlock {
+  int64_t row, block;
+  int v0, v1;            // its vectors
+  const T* z;
+  Cut<T> cut;
+  bool has_edge, edge_listed, bad;
+  int edge_at;
+  float edge;
+  Entry e;               // the first wavefront's
+  Listed listed;
+  float (*parts)[3];     // LDS
+  DistillStats* shared;  // LDS
+};
+
+// The row's loss and stats, and what its gradient takes in `b.shared` after the next barrier.
+template <bool REST, bool WIDE, typename T>
+__device__ __forceinline__ void distill_row_results(const DistillArgs& g, const DistillBlock<T>& b, Sums<WIDE> o, Scale<WIDE> k) {
+  if (threadIdx.x >= 64) return;
+  float loss;
+  DistillStats st;
+  distill_finish<REST>(b.e, o, k, g.scale, b.bad, loss, st);
+  if (threadIdx.x == 0) {
+    if (g.loss) g.loss[b.row] = loss;
+    g.stats[b.row] = st;
+    *b.shared = st;
+  }
+}
+
+// The sums over a row or a part, its logits from memory.
+template <int W, bool REST, bool WIDE, typename T>
+__device__ __forceinline__ Sums<WIDE> distill_sums(const DistillBlock<T>& b, Scale<WIDE> k, bool exact) {
+  constexpr int NT = 64 * W, N = RowTypes<T>::n;
+  Sums<WIDE> o;
+  for_batches<NT, false>(b.z, b.cut, b.v0, b.v1, [&](int i, const Packed<T>(&p)[kBatch]) {
+    Wide<T> x[kBatch];
+    float hi = kNone;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int v = i + u * NT;
+      x[u] = v < b.v1 ? widen<T>(p[u]) : Wide<T>(-__builtin_inff());
+      if (REST) leave_out<T>(x[u], b.listed.template marks<N>(v, b.cut.start(v), exact));
+      hi = fmaxf(hi, largest<T>(x[u]));
+    }
+    add_batch<false, WIDE, T>(o, k, x, hi);
+  });
+  if (b.has_edge && !b.edge_listed) o.template one<false>(b.edge, k);
+  return over_block<W>(o, k, b.parts);
+}
+
+// A row's gradient after its sums, its logits read again.
+template <int W, bool REST, bool WIDE, typename T>
+__device__ __forceinline__ void distill_write(const DistillArgs& g, const DistillBlock<T>& b, Sums<WIDE> o, Scale<WIDE> k) {
+  constexpr int NT = 64 * W, N = RowTypes<T>::n;
+  __syncthreads();
+  T* out = static_cast<T*>(g.grad) + b.row * g.grad_stride;
+  const float scaled = g.scale * g.grad_loss[b.row], f = b.shared->f * scaled;
+  auto one = [&](float x) { return exp2_hw(k.exponent(x, o.ref)) * f; };
+  for_batches<NT, false>(b.z, b.cut, 0, b.cut.nvec, [&](int i, const Packed<T>(&p)[kBatch]) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (i + u * NT >= b.cut.nvec) break;
+      Wide<T> x = widen<T>(p[u]);
+#pragma unroll
+      for (int n = 0; n < N; ++n) x[n] = one(x[n]);
+      store_packed(out + b.cut.start(i + u * NT), narrow<T>(x));
+    }
+  });
+  if (b.has_edge) out[b.edge_at] = (T)one(b.edge);
+  __syncthreads();
+  if (threadIdx.x < 64) patch_listed(g, out, b.e, scaled, *b.shared);
+}
+
+// Loss and gradient in one pass, a block a row, which stays in registers: NV vectors a thread.  (A row that is not
+// plain is read again.)
+template <typename T, int W, int NV, bool REST>
+__global__ __launch_bounds__(64 * W) void distill_row_kernel(DistillArgs g, uint32_t mask) {
+  constexpr int NT = 64 * W, N = RowTypes<T>::n, B = W == 16 ? 2 : kBatch;  // 1024 threads have 128 registers each
+  extern __shared__ uint32_t words[];
+  __shared__ float parts[W][3];
+  __shared__ int ids[65];
+  __shared__ DistillStats shared;
   const int64_t row = block_row();
   if (row >= g.rows) return;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
-  const float c = g.scale * kLog2e;
   const Cut<T> cut(z, g.vocab);
-  const DistillRow<T, REST> r{z, cut, g.vocab, g.entries, bitmap_mask, (uint32_t)cut.nvec <= bitmap_mask + 1,
-                              reinterpret_cast<const uint8_t*>(bitmap), listed};
-  bool bad = false;
-  Entry e{};
-  if (wave == 0) e = entry_of<T, REST>(g, z, row, lane, bad);
+  const Scale<false> k{g.scale * kLog2e};
+  Words p[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int v = (int)threadIdx.x + i * NT;  // past the row: its last vector again, which is then not used
+    p[i] = cut.nvec ? __builtin_nontemporal_load(reinterpret_cast<const Words*>(z + cut.head) + (v < cut.nvec ? v : cut.nvec - 1)) : Words(0);
+  }
+  DistillBlock<T> b{row, row, 0, cut.nvec, z, cut, (int)threadIdx.x < cut.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts, &shared};
+  b.edge_at = b.has_edge ? cut.edge(threadIdx.x) : 0;
+  b.edge = b.has_edge ? (float)z[b.edge_at] : -__builtin_inff();
+  if (threadIdx.x < 64) b.e = entry_of<T, REST>(g, z, row, threadIdx.x, b.bad);
+  bool huge = false;
   if constexpr (REST) {
-    for (uint32_t i = threadIdx.x; i <= bitmap_mask / 4; i += NT) bitmap[i] = 0;
-    __syncthreads();
-    if (wave == 0) {
-      listed[lane] = (int)e.id;
-      const int d = (int)e.id - cut.head;
-      if (e.id >= 0 && d >= 0 && d / N < cut.nvec) {
-        const uint32_t at = (d / N) & bitmap_mask;
-        atomicOr(&bitmap[at / 4], 1u << (at % 4 * 8 + d % N));
-      }
-    }
-    __syncthreads();
+    b.listed = list_entries<NT>(words, mask, ids, cut, b.e, g.entries, threadIdx.x < 64 && __any(huge_entry(b.e, k.c)));
+    b.edge_listed = b.has_edge && b.listed.has(b.edge_at);
+    huge = __builtin_amdgcn_readfirstlane(ids[64]);
   }
-  Online o;
-  for (int i = threadIdx.x; i < cut.nvec; i += NT) {
-    Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
-    if constexpr (REST) {
-      const uint32_t b = r.marks(i);
-      if (b) {
+  Sums<false> o;
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-          if (b >> k & 1) x[k] = -__builtin_inff();
-      }
-    }
-    float hi = x[0];
+  for (int i = 0; i < NV; i += B) {
+    Wide<T> x[B];
+    float hi = kNone;
 #pragma unroll
-    for (int k = 1; k < N; ++k) hi = fmaxf(hi, x[k]);
-    if (hi > o.m) o.rise(hi, c);
-#pragma unroll
-    for (int k = 0; k < N; ++k) o.s += exp2_hw((x[k] - o.m) * c);
-  }
-  if ((int)threadIdx.x < cut.edges) {
-    const int at = cut.edge(threadIdx.x);
-    if (!REST || !r.is_listed(at)) {
-      const float x = (float)z[at];
-      if (x > o.m) o.rise(x, c);
-      o.s += exp2_hw((x - o.m) * c);
+    for (int u = 0; u < B; ++u) {
+      const int v = (int)threadIdx.x + (i + u) * NT;
+      forget(p[i + u]);
+      x[u] = widen<T>(__builtin_bit_cast(Packed<T>, p[i + u]));
+      if ((i + u + 1) * NT > cut.nvec && v >= cut.nvec) x[u] = -__builtin_inff();
+      if (REST) leave_out<T>(x[u], b.listed.template marks<N>(v, cut.start(v), true));
+      hi = fmaxf(hi, largest<T>(x[u]));
     }
+    add_batch<false, false, T>(o, k, x, hi);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  o = block_join<kWaves>(o, c, parts);
-  if (wave == 0) {
-    const DistillResult d = distill_finish<REST>(e, o, g.scale, bad);
-    if (lane == 0) {
-      if (g.loss) g.loss[row] = d.loss;
-      if (g.stats) g.stats[row] = make_float4(o.m, d.f, d.m, d.lse);
-      result[0] = d.f;
-      result[1] = d.m;
-      result[2] = d.lse;
-      result[3] = d.total;
-    }
+  if (b.has_edge && !b.edge_listed) o.template one<false>(b.edge, k);
+  o = over_block<W>(o, k, parts);
+  if (huge || !plain(o.ref)) {
+    const Scale<true> kw{k.c};
+    const Sums<true> w = distill_sums<W, REST>(b, kw, true);
+    distill_row_results<REST>(g, b, w, kw);
+    distill_write<W, REST>(g, b, w, kw);
+    return;
   }
-  if (!g.grad) return;
+  distill_row_results<REST>(g, b, o, k);
   __syncthreads();
   T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
-  const float scaled = g.scale * g.grad_loss[row], f = result[0] * scaled;
-  auto one = [&](float x) { return exp2_hw((x - o.m) * c) * f; };
-  for (int i = threadIdx.x; i < cut.nvec; i += NT) {
-    Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
+  const float scaled = g.scale * g.grad_loss[row], f = shared.f * scaled;
+  auto one = [&](float x) { return exp2_hw(k.exponent(x, o.ref)) * f; };
 #pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = one(x[k]);
-    store_packed(out + cut.start(i), narrow<T>(x));
+  for (int i = 0; i < NV; ++i) {
+    forget(p[i]);
+    if ((int)threadIdx.x + i * NT < cut.nvec) {
+      Wide<T> x = widen<T>(__builtin_bit_cast(Packed<T>, p[i]));
+#pragma unroll
+      for (int n = 0; n < N; ++n) x[n] = one(x[n]);
+      store_packed(cut.of(out, i * NT), narrow<T>(x));
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  if ((int)threadIdx.x < cut.edges) {
-    const int at = cut.edge(threadIdx.x);
-    out[at] = (T)one((float)z[at]);
-  }
+  if (b.has_edge) out[b.edge_at] = (T)one(b.edge);
   __syncthreads();
-  if (wave == 0) patch_listed(g, out, e, scaled, result[3], result[1], result[2]);
+  if (threadIdx.x < 64) patch_listed(g, out, b.e, scaled, shared);
+}
+
+// The sums of one of a row's parts; with one part the row's loss and stats, and with `grad` its gradient, for which
+// the logits are read again (a row too long for registers: from the Infinity Cache).
+template <typename T, int W, bool REST>
+__global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs g, uint32_t mask) {
+  constexpr int NT = 64 * W;
+  extern __shared__ uint32_t words[];
+  __shared__ float parts[W][3];
+  __shared__ int ids[65];
+  __shared__ DistillStats shared;
+  const int64_t block = block_row();
+  if (block >= g.rows * g.parts) return;
+  const int64_t row = g.parts == 1 ? block : block / g.parts;
+  const int part = g.parts == 1 ? 0 : (int)(block % g.parts);
+  const T* z = static_cast<const T*>(g.logits) + row * g.stride;
+  const Cut<T> cut(z, g.vocab);
+  const Scale<false> k{g.scale * kLog2e};
+  DistillBlock<T> b{row, block, 0, 0, z, cut, part == 0 && (int)threadIdx.x < cut.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts,
+                    &shared};
+  b.v0 = (int)((int64_t)cut.nvec * part / g.parts);
+  b.v1 = (int)((int64_t)cut.nvec * (part + 1) / g.parts);
+  b.edge_at = b.has_edge ? cut.edge(threadIdx.x) : 0;
+  b.edge = b.has_edge ? (float)z[b.edge_at] : -__builtin_inff();
+  if (threadIdx.x < 64 && (REST || g.parts == 1)) b.e = entry_of<T, REST>(g, z, row, threadIdx.x, b.bad);
+  bool huge = false;
+  if constexpr (REST) {
+    b.listed = list_entries<NT>(words, mask, ids, cut, b.e, g.entries, threadIdx.x < 64 && __any(huge_entry(b.e, k.c)));
+    b.edge_listed = b.has_edge && b.listed.has(b.edge_at);
+    huge = __builtin_amdgcn_readfirstlane(ids[64]);
+  }
+  const bool exact = (uint32_t)cut.nvec <= mask + 1;
+  auto rest = [&](auto o, auto by) {
+    if (g.parts > 1) {
+      if (threadIdx.x == 0) g.part_sums[block] = make_float4(o.ref, o.s, 0.f, std::is_same_v<decltype(by), Scale<true>> ? 1.f : 0.f);
+      return;
+    }
+    distill_row_results<REST>(g, b, o, by);
+    if (g.grad) distill_write<W, REST>(g, b, o, by);
+  };
+  const Sums<false> o = distill_sums<W, REST>(b, k, exact);
+  if (plain(o.ref) && !huge) {
+    rest(o, k);
+  } else {
+    const Scale<true> kw{k.c};
+    rest(distill_sums<W, REST>(b, kw, exact), kw);
+  }
+}
+
+// A row's loss and stats from its parts' sums: a wavefront a row.
+template <typename T, bool REST>
+__global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
+  const int64_t row = block_row();
+  if (row >= g.rows) return;
+  const int lane = threadIdx.x;
+  const bool there = lane < g.parts;
+  const float4 sums = there ? g.part_sums[row * g.parts + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+  bool bad = false;
+  const Entry e = entry_of<T, REST>(g, static_cast<const T*>(g.logits) + row * g.stride, row, lane, bad);
+  float loss;
+  DistillStats st;
+  const float c = g.scale * kLog2e;
+  if (wide_row(there, sums, REST && huge_entry(e, c))) {
+    const Scale<true> k{c};
+    distill_finish<REST>(e, join_parts(there, sums, k), k, g.scale, bad, loss, st);
+  } else {
+    const Scale<false> k{c};
+    distill_finish<REST>(e, join_parts(there, sums, k), k, g.scale, bad, loss, st);
+  }
+  if (lane == 0) {
+    if (g.loss) g.loss[row] = loss;
+    if (g.stats) g.stats[row] = st;
+  }
 }
 
 template <typename T, bool REST>
 __global__ __launch_bounds__(64 * kWaves) void distill_grad_kernel(DistillArgs g) {
-  constexpr int NT = 64 * kWaves, N = RowTypes<T>::n;
-  const int64_t row = block_row();
-  if (row >= g.rows) return;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  constexpr int N = RowTypes<T>::n;
+  const int64_t block = block_row();
+  if (block >= g.rows * g.chunks) return;
+  const int64_t row = g.chunks == 1 ? block : block / g.chunks;
+  const int chunk = (int)(block - row * g.chunks), lane = threadIdx.x % 64;
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
-  const float c = g.scale * kLog2e;
   const Cut<T> cut(z, g.vocab);
-  const float4 st = g.stats[row];
-  const float scaled = g.scale * g.grad_loss[row], f = st.y * scaled, m = st.x;
+  const DistillStats st = g.stats[row];
+  const float scaled = g.scale * g.grad_loss[row], f = st.f * scaled;
   bool bad = false;
   Entry e{};
-  float total = 0.f;
-  if (wave == 0) {
+  if (threadIdx.x < 64) {
     e = entry_of<T, REST>(g, z, row, lane, bad);
-    total = wave_sum(e.q);
-    if (REST) total += fmaxf(1.f - total, 0.f);
+    const int d = e.id - cut.head, vec = d / N;  // entries of other chunks are theirs to write
+    const bool edge = d < 0 || vec >= cut.nvec;
+    if (edge ? chunk != 0 : vec / kChunk != chunk) e.id = -1;
   }
   __syncthreads();  // in place: the entries' logits are read before anything is written
-  auto one = [&](float x) { return exp2_hw((x - m) * c) * f; };
-  for (int i = threadIdx.x; i < cut.nvec; i += NT) {
-    Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
-#pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = one(x[k]);
-    store_packed(out + cut.start(i), narrow<T>(x));
-  }
-  if ((int)threadIdx.x < cut.edges) {
-    const int at = cut.edge(threadIdx.x);
-    out[at] = (T)one((float)z[at]);
-  }
+  auto run = [&](auto k) {
+    map_chunk(z, out, cut, chunk, [&](float x, int) { return exp2_hw(k.exponent(x, st.rest_ref)) * f; });
+  };
+  if (st.wide == 0.f) run(Scale<false>{g.scale * kLog2e});
+  else run(Scale<true>{g.scale * kLog2e});
   __syncthreads();
-  if (wave == 0) patch_listed(g, out, e, scaled, total, st.z, st.w);
+  if (threadIdx.x < 64) patch_listed(g, out, e, scaled, st);
+}
+
+uint32_t bitmap_bytes(int64_t vocab, int n, bool rest) {
+  uint32_t bytes = 64;
+  while (bytes < vocab / n + 1 && bytes < kBitmapMost) bytes *= 2;
+  return rest ? bytes : 64;
 }
 
 }  // namespace
@@ -644,47 +928,89 @@ int row_parts(int64_t rows, int64_t vocab) {
 hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream) {
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (g.vocab / RowTypes<T>::n <= 256)
-      HVDX_LAUNCH((logprobs_kernel<T, 1>), row_grid(g.rows * g.parts), dim3(64), 0, stream, g);
-    else
-      HVDX_LAUNCH((logprobs_kernel<T, kWaves>), row_grid(g.rows * g.parts), dim3(64 * kWaves), 0, stream, g);
+    const dim3 grid = row_grid(g.rows * g.parts);
+    if (g.vocab / RowTypes<T>::n <= 256) {
+      if (g.top) HVDX_LAUNCH((logprobs_kernel<T, 1, true>), grid, dim3(64), 0, stream, g);
+      else HVDX_LAUNCH((logprobs_kernel<T, 1, false>), grid, dim3(64), 0, stream, g);
+    } else {
+      if (g.top) HVDX_LAUNCH((logprobs_kernel<T, kWaves, true>), grid, dim3(64 * kWaves), 0, stream, g);
+      else HVDX_LAUNCH((logprobs_kernel<T, kWaves, false>), grid, dim3(64 * kWaves), 0, stream, g);
+    }
   });
   return hipGetLastError();
 }
 
 hipError_t launch_logprobs_join(const LogprobArgs& g, int dtype, hipStream_t stream) {
+  HVDX_LAUNCH(logprobs_join_kernel, row_grid(g.rows), dim3(64 * kWaves), 0, stream, g, dtype);
+  return hipGetLastError();
+}
+
+hipError_t launch_logprobs_grad(const LogprobGradArgs& args, int dtype, hipStream_t stream) {
   by_type(dtype, [&](auto t) {
-    HVDX_LAUNCH(logprobs_join_kernel<decltype(t)>, row_grid(g.rows), dim3(64 * kWaves), 0, stream, g);
+    using T = decltype(t);
+    LogprobGradArgs g = args;
+    g.chunks = row_chunks(g.vocab, RowTypes<T>::n);
+    HVDX_LAUNCH(logprobs_grad_kernel<T>, row_grid(g.rows * g.chunks), dim3(64 * kWaves), 0, stream, g);
   });
   return hipGetLastError();
 }
 
-hipError_t launch_logprobs_grad(const LogprobGradArgs& g, int dtype, hipStream_t stream) {
-  by_type(dtype, [&](auto t) {
-    HVDX_LAUNCH(logprobs_grad_kernel<decltype(t)>, row_grid(g.rows), dim3(64 * kWaves), 0, stream, g);
-  });
-  return hipGetLastError();
+int distill_parts(int64_t rows, int64_t vocab, int dtype, bool grad) {
+  if (grad && vocab / (dtype == HVDX_FLOAT32 ? 4 : 8) <= kRowMost) return 1;
+  return row_parts(rows, vocab);
 }
 
 hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream) {
-  const int64_t vectors = g.vocab / (dtype == HVDX_FLOAT32 ? 4 : 8) + 1;
-  uint32_t bytes = 64;
-  while (bytes < vectors && bytes < (uint32_t)kBitmapMost) bytes *= 2;
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (g.rest)
-      HVDX_LAUNCH((distill_kernel<T, true>), row_grid(g.rows), dim3(64 * kWaves), bytes, stream, g, bytes - 1);
-    else
-      HVDX_LAUNCH((distill_kernel<T, false>), row_grid(g.rows), dim3(64 * kWaves), 0, stream, g, 0u);
+    const int64_t vectors = g.vocab / RowTypes<T>::n;
+    const uint32_t bytes = bitmap_bytes(g.vocab, RowTypes<T>::n, g.rest);
+    auto pass = [&](auto w) {
+      constexpr int W = w();
+      const dim3 grid = row_grid(g.rows * g.parts), threads(64 * W);
+      if (g.rest) HVDX_LAUNCH((distill_kernel<T, W, true>), grid, threads, bytes, stream, g, bytes - 1);
+      else HVDX_LAUNCH((distill_kernel<T, W, false>), grid, threads, bytes, stream, g, bytes - 1);
+    };
+    auto row = [&](auto w, auto nv) {
+      constexpr int W = w(), NV = nv();
+      const dim3 grid = row_grid(g.rows), threads(64 * W);
+      if (g.rest) HVDX_LAUNCH((distill_row_kernel<T, W, NV, true>), grid, threads, bytes, stream, g, bytes - 1);
+      else HVDX_LAUNCH((distill_row_kernel<T, W, NV, false>), grid, threads, bytes, stream, g, bytes - 1);
+    };
+    using std::integral_constant;
+#define HVDX_ROW(w, nv) row(integral_constant<int, w>{}, integral_constant<int, nv>{})
+    if (g.parts > 1 || !g.grad) {
+      if (vectors <= 256) pass(integral_constant<int, 1>{});
+      else pass(integral_constant<int, kWaves>{});
+    } else if (vectors <= 256) HVDX_ROW(1, 4);
+    else if (vectors <= 1024) HVDX_ROW(4, 4);
+    else if (vectors <= 2048) HVDX_ROW(4, 8);
+    else if (vectors <= 4096) HVDX_ROW(8, 8);
+    else if (vectors <= 8192) HVDX_ROW(8, 16);
+    else if (vectors <= kRowMost) HVDX_ROW(16, 16);
+    else pass(integral_constant<int, 16>{});
+#undef HVDX_ROW
   });
   return hipGetLastError();
 }
 
-hipError_t launch_distill_grad(const DistillArgs& g, int dtype, hipStream_t stream) {
+hipError_t launch_distill_join(const DistillArgs& g, int dtype, hipStream_t stream) {
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (g.rest) HVDX_LAUNCH((distill_grad_kernel<T, true>), row_grid(g.rows), dim3(64 * kWaves), 0, stream, g);
-    else HVDX_LAUNCH((distill_grad_kernel<T, false>), row_grid(g.rows), dim3(64 * kWaves), 0, stream, g);
+    if (g.rest) HVDX_LAUNCH((distill_join_kernel<T, true>), row_grid(g.rows), dim3(64), 0, stream, g);
+    else HVDX_LAUNCH((distill_join_kernel<T, false>), row_grid(g.rows), dim3(64), 0, stream, g);
+  });
+  return hipGetLastError();
+}
+
+hipError_t launch_distill_grad(const DistillArgs& args, int dtype, hipStream_t stream) {
+  by_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    DistillArgs g = args;
+    g.chunks = row_chunks(g.vocab, RowTypes<T>::n);
+    const dim3 grid = row_grid(g.rows * g.chunks), threads(64 * kWaves);
+    if (g.rest) HVDX_LAUNCH((distill_grad_kernel<T, true>), grid, threads, 0, stream, g);
+    else HVDX_LAUNCH((distill_grad_kernel<T, false>), grid, threads, 0, stream, g);
   });
   return hipGetLastError();
 }

@@ -145,7 +145,7 @@ class DistillLoss(_Operator):
         self.rows, self.vocab, self.alternatives, self.rest = rows, vocab, alternatives, bool(rest)
         self.device = _device(device)
         self._bytes = L.hvdx_distill_workspace_bytes(rows, vocab)
-        self._own(self.device, loss=torch.empty(rows, device=self.device), stats=torch.empty(rows, 4, device=self.device),
+        self._own(self.device, loss=torch.empty(rows, device=self.device), stats=torch.empty(rows, 8, device=self.device),
                   workspace=torch.empty(self._bytes, dtype=torch.uint8, device=self.device))
         self.scale = None  # the last call's
 
