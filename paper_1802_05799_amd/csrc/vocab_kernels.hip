@@ -156,50 +156,56 @@ __device__ __forceinline__ int key_position(uint64_t k) { return (int)~(uint32_t
 constexpr int kWaves = 4;
 
 // The `k` first of a block's keys.  Each thread has the first of its own as `best`, at a coarser grain
-// (the position of its vector); the block's 64 groups of W threads have one first key each, and the
-// k-th of those is a bound that at least k keys reach: what lies below it cannot be among the k
-// first.  Little reaches it (k = 32 of 131,072 normal values: about 45), so the threads with any
-// collect those into LDS, where each finds its rank by counting.  Where more reach it than LDS
-// holds, k rounds over all keys find them one by one.
-constexpr int kCandidates = 1024;
+// (the position of its vector); the k-th of the first keys of G groups of threads is a bound that at least k
+// keys reach: what lies below it cannot be among the k first.  Little reaches it: -G ln(1 - k/G)
+// keys where they lie at random, so G is some four times k.  The threads collect those into LDS, where each
+// finds its rank by counting.  Where more reach it than LDS holds, k rounds over all keys find them one
+// by one.
+constexpr int kCandidates = 512;
 template <int W>
 struct TopLds {
-  uint64_t group[64], candidate[kCandidates], best[W], bound;
-  int count;
+  uint64_t group[64 * W], candidate[kCandidates], best[W], bound;
+  int count, items;
 };
-template <int W, typename Collect, typename Below, typename Emit>
-__device__ void select_top(int k, uint64_t best, TopLds<W>& lds, Collect collect, Below below, Emit emit) {
-  constexpr int NT = 64 * W;
+template <int W>
+__device__ __forceinline__ uint64_t top_bound(int k, uint64_t best, TopLds<W>& lds) {  // ends with a barrier
   const int tid = threadIdx.x;
+  int groups = 64, span = W;  // groups of `span` threads
+  while (span > 1 && groups < 4 * k) groups *= 2, span /= 2;
   uint64_t first = best;
-#pragma unroll
-  for (int j = 1; j < W; j *= 2) {
+  for (int j = 1; j < span; j *= 2) {
     const uint64_t other = __shfl_xor((unsigned long long)first, j);
     if (other > first) first = other;
   }
-  if (tid % W == 0) lds.group[tid / W] = first;
-  if (tid == 0) lds.count = 0;
+  if (tid % span == 0) lds.group[tid / span] = first;
+  if (tid == 0) lds.count = lds.items = 0;
   __syncthreads();
-  if (tid < 64) {
+  if (tid < groups) {
     const uint64_t mine = lds.group[tid];
     int rank = 0;
 #pragma unroll 16
-    for (int j = 0; j < 64; ++j) {
+    for (int j = 0; j < groups; ++j) {
       const uint64_t other = lds.group[j];
       rank += other > mine || (other == mine && j < tid);
     }
     if (rank == k - 1) lds.bound = mine;
   }
   __syncthreads();
-  const uint64_t bound = lds.bound;
-  if (best && best >= bound)
-    collect(bound, [&](uint64_t key) {
-      const int at = atomicAdd(&lds.count, 1);
-      if (at < kCandidates) lds.candidate[at] = key;
-    });
+  return lds.bound;
+}
+template <int W>
+__device__ __forceinline__ void top_push(TopLds<W>& lds, uint64_t key) {
+  const int at = atomicAdd(&lds.count, 1);
+  if (at < kCandidates) lds.candidate[at] = key;
+}
+// Ranks what was pushed; `complete`: nothing was left out of it for want of space elsewhere.
+template <int W, typename Below, typename Emit>
+__device__ __forceinline__ void top_finish(int k, TopLds<W>& lds, bool complete, Below below, Emit emit) {
+  constexpr int NT = 64 * W;
+  const int tid = threadIdx.x;
   __syncthreads();
   const int count = lds.count;
-  if (count <= kCandidates) {
+  if (complete && count <= kCandidates) {
     for (int i = tid; i < count; i += NT) {
       const uint64_t mine = lds.candidate[i];
       int rank = 0;
@@ -259,15 +265,19 @@ __device__ __forceinline__ void emit_top(const LogprobArgs& g, int64_t row, int 
 // first keys go to the workspace for logprobs_join_kernel.
 //
 // For the alternatives a thread notes the largest of its elements, and in LDS the largest of each of kNotes
-// stretches of its vectors: of the stretches that reach the bound it reads its own again, and no
-// others.  (Reading all its vectors again, 16 bytes of each line, cost as much as the pass itself.)
-constexpr int kNotes = 16;
+// stretches of its vectors.  The stretches that reach the bound are listed, and all threads together read
+// their vectors again.  (Threads reading all of theirs again, 16 bytes of each line, cost as much as the
+// pass; threads reading their own stretches, one after the other, as much in latency.)  A single
+// wavefront's row is one batch, which is still in registers.
+constexpr int kNotes = 16, kItems = 1024;
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
   constexpr int NT = 64 * W, N = RowTypes<T>::n;
+  constexpr bool NOTES = TOP && W > 1;
   __shared__ float parts[W][3];
   __shared__ TopLds<TOP ? W : 1> top;
-  __shared__ float notes[TOP ? kNotes : 1][TOP ? NT : 1];
+  __shared__ float notes[NOTES ? kNotes : 1][NOTES ? NT : 1];
+  __shared__ int items[NOTES ? kItems : 1];  // stretch * NT + thread
   const int64_t block = block_row();
   if (block >= g.rows * g.parts) return;
   const int64_t row = g.parts == 1 ? block : block / g.parts;
@@ -288,8 +298,8 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
   const int batches = (v1 - v0 + kBatch * NT - 1) / (kBatch * NT), per_note = (batches + kNotes - 1) / kNotes;
   int note = 0, left = per_note;
   float noted = -__builtin_inff();
+  Wide<T> x[kBatch];
   for_batches<NT, !TOP>(z, cut, v0, v1, [&](int i, const Packed<T>(&p)[kBatch]) {
-    Wide<T> x[kBatch];
     float hi = kNone;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -302,7 +312,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
       hi = fmaxf(hi, h);
     }
     add_batch<true, false, T>(o, k, x, hi);
-    if constexpr (TOP) {
+    if constexpr (NOTES) {
       noted = fmaxf(noted, hi);
       notes[note][threadIdx.x] = noted;
       if (--left == 0) {
@@ -313,7 +323,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
     }
   });
   if (has_edge) {
-    o.one<true>(edge, k);
+    o.template one<true>(edge, k);
     if (TOP && (high_at < 0 || key_of(edge, edge_at) > key_of(high, high_at))) {  // it may stand before the vectors
       high = edge;
       high_at = edge_at;
@@ -328,10 +338,10 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
     const Scale<true> kw{k.c};
     Sums<true> w;
     for (int i = v0 + threadIdx.x; i < v1; i += NT) {
-      const Wide<T> x[1] = {widen<T>(load_packed(z + cut.start(i)))};
-      add_batch<true, true, T>(w, kw, x, largest<T>(x[0]));
+      const Wide<T> y[1] = {widen<T>(load_packed(z + cut.start(i)))};
+      add_batch<true, true, T>(w, kw, y, largest<T>(y[0]));
     }
-    if (has_edge) w.one<true>(edge, kw);
+    if (has_edge) w.template one<true>(edge, kw);
     w = over_block<W>(w, kw, parts);
     r = row_sums(w);
     sums = make_float4(w.ref, w.s, w.a, 1.f);
@@ -342,39 +352,52 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
     else g.part_sums[block] = sums;
   }
   if constexpr (TOP) {
-    select_top<W>(
-        g.top, high_at < 0 ? 0 : key_of(high, high_at), top,
-        [&](uint64_t bound, auto push) {
-          const float least = key_value(bound);
-          int n = 0;
-          for (int b = 0; b < batches; ++n) {
-            const int end = b + per_note < batches ? b + per_note : batches;
-            if (bound && v0 + (int)threadIdx.x + b * kBatch * NT < v1 && notes[n][threadIdx.x] < least) {
-              b = end;
-              continue;
-            }
-            for (int i = v0 + threadIdx.x + b * kBatch * NT; i < v1 && i < v0 + end * kBatch * NT; i += NT) {
-              const int start = cut.start(i);
-              const Wide<T> x = widen<T>(load_packed(z + start));
-              if (key_of(largest<T>(x), start) < bound) continue;
+    const uint64_t best = high_at < 0 ? 0 : key_of(high, high_at), bound = top_bound<W>(g.top, best, top);
+    auto search = [&](const Wide<T>& y, int start) {
+      if (key_of(largest<T>(y), start) < bound) return;
 #pragma unroll
-              for (int e = 0; e < N; ++e)
-                if (key_of(x[e], start) >= bound) push(key_of(x[e], start + e));
-            }
-            b = end;
-          }
-          if (has_edge && key_of(edge, edge_at) >= bound) push(key_of(edge, edge_at));
-        },
+      for (int e = 0; e < N; ++e)
+        if (key_of(y[e], start) >= bound) top_push(top, key_of(y[e], start + e));
+    };
+    const bool mine = best && best >= bound;
+    bool complete = true;
+    if (mine && has_edge && key_of(edge, edge_at) >= bound) top_push(top, key_of(edge, edge_at));
+    if constexpr (NOTES) {
+      if (mine) {
+        const float least = bound ? key_value(bound) : -__builtin_inff();
+        for (int n = 0; n < kNotes; ++n) {
+          if (v0 + (int)threadIdx.x + n * per_note * kBatch * NT >= v1) break;
+          if (notes[n][threadIdx.x] < least) continue;
+          const int at = atomicAdd(&top.items, 1);
+          if (at < kItems) items[at] = n * NT + threadIdx.x;
+        }
+      }
+      __syncthreads();
+      const int stretch = per_note * kBatch;
+      complete = top.items <= kItems;
+      const int vectors = (complete ? top.items : 0) * stretch;
+      for (int i = threadIdx.x; i < vectors; i += NT) {
+        const int item = items[i / stretch];
+        const int v = v0 + item % NT + (item / NT * stretch + i % stretch) * NT;
+        if (v < v1) search(widen<T>(load_packed(z + cut.start(v))), cut.start(v));
+      }
+    } else if (mine) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (v0 + (int)threadIdx.x + u * NT < v1) search(x[u], cut.start(v0 + threadIdx.x + u * NT));
+    }
+    top_finish<W>(
+        g.top, top, complete,
         [&](uint64_t last) {
           uint64_t next = 0;
-          auto take = [&](float x, int at) {
-            const uint64_t key = key_of(x, at);
+          auto take = [&](float y, int at) {
+            const uint64_t key = key_of(y, at);
             if (key < last && key > next) next = key;
           };
           for (int i = v0 + threadIdx.x; i < v1; i += NT) {
-            const Wide<T> x = widen<T>(load_packed(z + cut.start(i)));
+            const Wide<T> y = widen<T>(load_packed(z + cut.start(i)));
 #pragma unroll
-            for (int e = 0; e < N; ++e) take(x[e], cut.start(i) + e);
+            for (int e = 0; e < N; ++e) take(y[e], cut.start(i) + e);
           }
           if (has_edge) take(edge, edge_at);
           return next;
@@ -427,12 +450,12 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs 
                                                 : row_sums(join_parts<false>(there, sums, Scale<false>{c}));
   if (threadIdx.x == 0) finish_logprobs(g, row, z_token, token, r);
   if (!g.top) return;
-  select_top<kWaves>(
-      g.top, best, top,
-      [&](uint64_t bound, auto push) {
-        for (int i = threadIdx.x; i < nkeys; i += NT)
-          if (keys[i] && keys[i] >= bound) push(keys[i]);
-      },
+  const uint64_t bound = top_bound<kWaves>(g.top, best, top);
+  if (best && best >= bound)
+    for (int i = threadIdx.x; i < nkeys; i += NT)
+      if (keys[i] && keys[i] >= bound) top_push(top, keys[i]);
+  top_finish<kWaves>(
+      g.top, top, true,
       [&](uint64_t last) {
         uint64_t next = 0;
         for (int i = threadIdx.x; i < nkeys; i += NT)
@@ -734,8 +757,8 @@ __device__ __forceinline__ void distill_write(const DistillArgs& g, const Distil
 // Loss and gradient in one pass, a block a row, which stays in registers: NV vectors a thread.  (A row that is not
 // plain is read again.)
 template <typename T, int W, int NV, bool REST>
-__global__ __launch_bounds__(64 * W) void distill_row_kernel(DistillArgs g, uint32_t mask) {
-  constexpr int NT = 64 * W, N = RowTypes<T>::n, B = W == 16 ? 2 : kBatch;  // 1024 threads have 128 registers each
+__global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g, uint32_t mask) {
+  constexpr int NT = 64 * W, N = RowTypes<T>::n, B = NV == 16 ? 2 : kBatch;  // there are 128 registers for a thread
   extern __shared__ uint32_t words[];
   __shared__ float parts[W][3];
   __shared__ int ids[65];
@@ -929,7 +952,7 @@ hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream) 
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const dim3 grid = row_grid(g.rows * g.parts);
-    if (g.vocab / RowTypes<T>::n <= 256) {
+    if (g.vocab / RowTypes<T>::n <= 64 * kBatch) {  // one batch of one wavefront
       if (g.top) HVDX_LAUNCH((logprobs_kernel<T, 1, true>), grid, dim3(64), 0, stream, g);
       else HVDX_LAUNCH((logprobs_kernel<T, 1, false>), grid, dim3(64), 0, stream, g);
     } else {
