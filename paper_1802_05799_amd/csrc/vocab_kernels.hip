@@ -535,21 +535,25 @@ struct Entry {
   float q_token;  // the probability of all of them
 };
 
-template <typename T, bool REST>
-__device__ __forceinline__ Entry entry_of(const DistillArgs& g, const T* z, int64_t row, int lane, bool& bad) {
+// Loaded first (load_entry), made of that (entry_of), and its logit last (entry_logit), so that a row's own loads
+// can be issued in between.
+struct LoadedEntry {
+  int64_t id;
+  float t;
+};
+__device__ __forceinline__ LoadedEntry load_entry(const DistillArgs& g, int64_t row, int lane) {
+  if (lane >= g.entries) return {-1, 0.f};
+  return {g.ids[row * g.entries + lane], g.teacher[row * g.entries + lane]};
+}
+template <bool REST>
+__device__ __forceinline__ Entry entry_of(const DistillArgs& g, LoadedEntry in, int lane, bool& bad) {
   Entry e{-1, 0.f, 0.f, 0.f, true, 0.f};
   float t = -__builtin_inff();
-  bool outside = false;
-  if (lane < g.entries) {
-    const int64_t id = g.ids[row * g.entries + lane];
-    outside = id >= g.vocab;
-    if (id >= 0 && !outside) {
-      e.id = (int)id;
-      t = g.teacher[row * g.entries + lane];
-      e.z = (float)z[id];
-    }
+  bad = __any(in.id >= g.vocab);
+  if (in.id >= 0 && in.id < g.vocab) {
+    e.id = (int)in.id;
+    t = in.t;
   }
-  bad = __any(outside);
   if constexpr (!REST) {
     const float high = wave_max(t);
     const float x = high == -__builtin_inff() ? t : t - high;
@@ -569,6 +573,11 @@ __device__ __forceinline__ Entry entry_of(const DistillArgs& g, const T* z, int6
   return e;
 }
 
+template <typename T>
+__device__ __forceinline__ float entry_logit(const Entry& e, const T* z) {
+  return e.id >= 0 ? (float)z[e.id] : 0.f;
+}
+
 // With `rest`, what is left of the teacher's mass, q_R, stands against the unlisted tokens' p_R, whose sum is taken
 // over them alone (subtracting the listed ones' from the whole would lose it where they hold nearly
 // everything): the pass leaves the listed tokens out, which a bitmap in LDS marks, a byte for each
@@ -581,11 +590,13 @@ constexpr int64_t kRowMost = 16384;
 struct Listed {
   const uint8_t* bitmap;
   uint32_t mask;
+  int threads, each;  // with `each`: a thread's bytes, for its every vector, lie together
   const int* ids;  // LDS, -1 for absent entries
   int entries;
+  __device__ uint32_t place(int vec) const { return each ? vec % threads * each + vec / threads : vec & mask; }
   template <int N>
   __device__ uint32_t marks(int vec, int start, bool exact) const {
-    uint32_t b = bitmap[vec & mask];
+    uint32_t b = bitmap[place(vec)];
     if (b && !exact) {
       b = 0;
       for (int j = 0; j < entries; ++j)
@@ -599,25 +610,24 @@ struct Listed {
     return false;
   }
 };
-// The block's bitmap of a row's entries; `ids` [65] and the words are LDS, ids[64] says whether one is `huge`.
-// Ends with a barrier.
-template <int NT, typename T>
+// The block's bitmap of a row's entries; `ids` [64] and the words are LDS.  Ends with a barrier.
+template <int NT, int NV = 0, typename T>
 __device__ __forceinline__ Listed list_entries(uint32_t* words, uint32_t mask, int* ids, const Cut<T>& cut, const Entry& e,
-                                               int entries, bool huge) {
+                                               int entries) {
   constexpr int N = RowTypes<T>::n;
+  const Listed listed{reinterpret_cast<const uint8_t*>(words), mask, NT, NV, ids, entries};
   for (uint32_t i = threadIdx.x; i <= mask / 4; i += NT) words[i] = 0;
   __syncthreads();
   if (threadIdx.x < 64) {
     ids[threadIdx.x] = e.id;
-    if (threadIdx.x == 0) ids[64] = huge;
     const int d = e.id - cut.head;
     if (e.id >= 0 && d >= 0 && d / N < cut.nvec) {
-      const uint32_t at = (uint32_t)(d / N) & mask;
+      const uint32_t at = listed.place(d / N);
       atomicOr(&words[at / 4], 1u << (at % 4 * 8 + d % N));
     }
   }
   __syncthreads();
-  return Listed{reinterpret_cast<const uint8_t*>(words), mask, ids, entries};
+  return listed;
 }
 template <typename T>
 __device__ __forceinline__ void leave_out(Wide<T>& x, uint32_t marks) {
@@ -630,6 +640,12 @@ __device__ __forceinline__ void leave_out(Wide<T>& x, uint32_t marks) {
 
 // Whether a listed token's logit makes its row WIDE, though the unlisted ones' would not.
 __device__ __forceinline__ bool huge_entry(const Entry& e, float c) { return e.id >= 0 && !(e.z * c < kPlain); }
+template <bool REST>
+__device__ __forceinline__ void note_huge(const Entry& e, float c, int* ids) {  // ids[64], for after the next barrier
+  if (!REST || threadIdx.x >= 64) return;
+  const bool any = __any(huge_entry(e, c));
+  if (threadIdx.x == 0) ids[64] = any;
+}
 
 // The row's loss and what its gradient takes, from the pass over the unlisted (REST) or all tokens.
 template <bool REST, bool WIDE>
@@ -754,12 +770,12 @@ __device__ __forceinline__ void distill_write(const DistillArgs& g, const Distil
   if (threadIdx.x < 64) patch_listed(g, out, b.e, scaled, *b.shared);
 }
 
-// Loss and gradient in one pass, a block a row, which stays in registers: NV vectors a thread.  (A row that is not
-// plain is read again.)
+// Loss and gradient in one pass, a block a row of at least one whole vector, which stays in registers: NV vectors a
+// thread.  (A row that is not plain is read again.)
 template <typename T, int W, int NV, bool REST>
-__global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g, uint32_t mask) {
+__global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g) {
   constexpr int NT = 64 * W, N = RowTypes<T>::n, B = NV == 16 ? 2 : kBatch;  // there are 128 registers for a thread
-  extern __shared__ uint32_t words[];
+  __shared__ uint32_t words[REST ? NT * NV / 4 : 1];
   __shared__ float parts[W][3];
   __shared__ int ids[65];
   __shared__ DistillStats shared;
@@ -768,22 +784,29 @@ __global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g, u
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   const Cut<T> cut(z, g.vocab);
   const Scale<false> k{g.scale * kLog2e};
+  DistillBlock<T> b{row, row, 0, cut.nvec, z, cut, (int)threadIdx.x < cut.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts, &shared};
+  // what is needed first is loaded before the row, behind which it would wait, and without a branch, at whose end
+  // it would be waited for
+  LoadedEntry in{};
+  if (threadIdx.x < 64) in = load_entry(g, row, threadIdx.x);
+  b.edge_at = b.has_edge ? cut.edge(threadIdx.x) : 0;
+  const T edge = z[b.edge_at];
   Words p[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int v = (int)threadIdx.x + i * NT;  // past the row: its last vector again, which is then not used
-    p[i] = cut.nvec ? __builtin_nontemporal_load(reinterpret_cast<const Words*>(z + cut.head) + (v < cut.nvec ? v : cut.nvec - 1)) : Words(0);
+    p[i] = __builtin_nontemporal_load(reinterpret_cast<const Words*>(z + cut.head) + (v < cut.nvec ? v : cut.nvec - 1));
   }
-  DistillBlock<T> b{row, row, 0, cut.nvec, z, cut, (int)threadIdx.x < cut.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts, &shared};
-  b.edge_at = b.has_edge ? cut.edge(threadIdx.x) : 0;
-  b.edge = b.has_edge ? (float)z[b.edge_at] : -__builtin_inff();
-  if (threadIdx.x < 64) b.e = entry_of<T, REST>(g, z, row, threadIdx.x, b.bad);
-  bool huge = false;
+  b.e.id = threadIdx.x < 64 && in.id >= 0 && in.id < g.vocab ? (int)in.id : -1;
+  const T logit = z[b.e.id >= 0 ? b.e.id : 0];
+  uint32_t marks[NV / 4] = {};
   if constexpr (REST) {
-    b.listed = list_entries<NT>(words, mask, ids, cut, b.e, g.entries, threadIdx.x < 64 && __any(huge_entry(b.e, k.c)));
+    b.listed = list_entries<NT, NV>(words, NT * NV - 1, ids, cut, b.e, g.entries);
     b.edge_listed = b.has_edge && b.listed.has(b.edge_at);
-    huge = __builtin_amdgcn_readfirstlane(ids[64]);
+#pragma unroll
+    for (int i = 0; i < NV / 4; ++i) marks[i] = words[threadIdx.x * (NV / 4) + i];
   }
+  if (threadIdx.x < 64) b.e = entry_of<REST>(g, in, threadIdx.x, b.bad);
   Sums<false> o;
 #pragma unroll
   for (int i = 0; i < NV; i += B) {
@@ -795,15 +818,18 @@ __global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g, u
       forget(p[i + u]);
       x[u] = widen<T>(__builtin_bit_cast(Packed<T>, p[i + u]));
       if ((i + u + 1) * NT > cut.nvec && v >= cut.nvec) x[u] = -__builtin_inff();
-      if (REST) leave_out<T>(x[u], b.listed.template marks<N>(v, cut.start(v), true));
+      if (REST) leave_out<T>(x[u], marks[(i + u) / 4] >> (i + u) % 4 * 8 & 0xff);
       hi = fmaxf(hi, largest<T>(x[u]));
     }
     add_batch<false, false, T>(o, k, x, hi);
     __builtin_amdgcn_sched_barrier(0);
   }
+  b.edge = b.has_edge ? (float)edge : -__builtin_inff();
+  b.e.z = b.e.id >= 0 ? (float)logit : 0.f;
   if (b.has_edge && !b.edge_listed) o.template one<false>(b.edge, k);
+  note_huge<REST>(b.e, k.c, ids);
   o = over_block<W>(o, k, parts);
-  if (huge || !plain(o.ref)) {
+  if (!plain(o.ref) || (REST && __builtin_amdgcn_readfirstlane(ids[64]))) {
     const Scale<true> kw{k.c};
     const Sums<true> w = distill_sums<W, REST>(b, kw, true);
     distill_row_results<REST>(g, b, w, kw);
@@ -853,13 +879,16 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs g, uint32_t
   b.v1 = (int)((int64_t)cut.nvec * (part + 1) / g.parts);
   b.edge_at = b.has_edge ? cut.edge(threadIdx.x) : 0;
   b.edge = b.has_edge ? (float)z[b.edge_at] : -__builtin_inff();
-  if (threadIdx.x < 64 && (REST || g.parts == 1)) b.e = entry_of<T, REST>(g, z, row, threadIdx.x, b.bad);
-  bool huge = false;
-  if constexpr (REST) {
-    b.listed = list_entries<NT>(words, mask, ids, cut, b.e, g.entries, threadIdx.x < 64 && __any(huge_entry(b.e, k.c)));
-    b.edge_listed = b.has_edge && b.listed.has(b.edge_at);
-    huge = __builtin_amdgcn_readfirstlane(ids[64]);
+  if (threadIdx.x < 64 && (REST || g.parts == 1)) {
+    b.e = entry_of<REST>(g, load_entry(g, row, threadIdx.x), threadIdx.x, b.bad);
+    b.e.z = entry_logit(b.e, z);
   }
+  note_huge<REST>(b.e, k.c, ids);
+  if constexpr (REST) {
+    b.listed = list_entries<NT>(words, mask, ids, cut, b.e, g.entries);
+    b.edge_listed = b.has_edge && b.listed.has(b.edge_at);
+  }
+  const bool huge = REST && __builtin_amdgcn_readfirstlane(ids[64]);
   const bool exact = (uint32_t)cut.nvec <= mask + 1;
   auto rest = [&](auto o, auto by) {
     if (g.parts > 1) {
@@ -887,7 +916,8 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
   const bool there = lane < g.parts;
   const float4 sums = there ? g.part_sums[row * g.parts + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
   bool bad = false;
-  const Entry e = entry_of<T, REST>(g, static_cast<const T*>(g.logits) + row * g.stride, row, lane, bad);
+  Entry e = entry_of<REST>(g, load_entry(g, row, lane), lane, bad);
+  e.z = entry_logit(e, static_cast<const T*>(g.logits) + row * g.stride);
   float loss;
   DistillStats st;
   const float c = g.scale * kLog2e;
@@ -919,7 +949,8 @@ __global__ __launch_bounds__(64 * kWaves) void distill_grad_kernel(DistillArgs g
   bool bad = false;
   Entry e{};
   if (threadIdx.x < 64) {
-    e = entry_of<T, REST>(g, z, row, lane, bad);
+    e = entry_of<REST>(g, load_entry(g, row, lane), lane, bad);
+    e.z = entry_logit(e, z);
     const int d = e.id - cut.head, vec = d / N;  // entries of other chunks are theirs to write
     const bool edge = d < 0 || vec >= cut.nvec;
     if (edge ? chunk != 0 : vec / kChunk != chunk) e.id = -1;
@@ -997,12 +1028,12 @@ hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream) {
     auto row = [&](auto w, auto nv) {
       constexpr int W = w(), NV = nv();
       const dim3 grid = row_grid(g.rows), threads(64 * W);
-      if (g.rest) HVDX_LAUNCH((distill_row_kernel<T, W, NV, true>), grid, threads, bytes, stream, g, bytes - 1);
-      else HVDX_LAUNCH((distill_row_kernel<T, W, NV, false>), grid, threads, bytes, stream, g, bytes - 1);
+      if (g.rest) HVDX_LAUNCH((distill_row_kernel<T, W, NV, true>), grid, threads, 0, stream, g);
+      else HVDX_LAUNCH((distill_row_kernel<T, W, NV, false>), grid, threads, 0, stream, g);
     };
     using std::integral_constant;
 #define HVDX_ROW(w, nv) row(integral_constant<int, w>{}, integral_constant<int, nv>{})
-    if (g.parts > 1 || !g.grad) {
+    if (g.parts > 1 || !g.grad || vectors < 2) {  // fewer may hold no vector on its boundary
       if (vectors <= 256) pass(integral_constant<int, 1>{});
       else pass(integral_constant<int, kWaves>{});
     } else if (vectors <= 256) HVDX_ROW(1, 4);
