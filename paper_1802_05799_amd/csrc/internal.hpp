@@ -261,7 +261,7 @@ struct LogprobArgs {
   float4* stats;  // reference, log2 of the sum, entropy, 1 where the reference is unscaled
   int parts;      // blocks a row (row_parts); with more than one:
   float4* part_sums;    // [rows][parts]
-  uint64_t* part_keys;  // [rows][parts][top]
+  uint64_t* part_keys;  // [rows][top][parts]
 };
 int row_parts(int64_t rows, int64_t vocab);
 hipError_t launch_logprobs_join(const LogprobArgs& g, int dtype, hipStream_t stream);  // after the other, with parts > 1

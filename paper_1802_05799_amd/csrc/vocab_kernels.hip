@@ -15,8 +15,8 @@ namespace hvdx {
 namespace {
 
 // Rows are split over blocks where there are too few of them to fill the chip: into parts of at least
-// kPartLeast elements, until there are kBlocksWanted blocks.
-constexpr int64_t kBlocksWanted = 1024, kPartLeast = 4096;
+// kPartLeast elements (a batch of a block's threads, in 16 bits), until there are kBlocksWanted blocks.
+constexpr int64_t kBlocksWanted = 512, kPartLeast = 8192;
 constexpr int kPartsMost = 64;  // one lane each when they are joined
 
 constexpr float kNone = -3.402823466e38f;  // the reference of nothing: finite, so that -inf minus it is no NaN
@@ -178,16 +178,16 @@ __device__ __forceinline__ uint64_t top_bound(int k, uint64_t best, TopLds<W>& l
     if (other > first) first = other;
   }
   if (tid % span == 0) lds.group[tid / span] = first;
-  if (tid == 0) lds.count = lds.items = 0;
+  if (tid == 0) {
+    lds.count = lds.items = 0;
+    lds.bound = 0;  // where fewer than k groups have any: keys differ, but for the 0 of those that have none
+  }
   __syncthreads();
   if (tid < groups) {
     const uint64_t mine = lds.group[tid];
     int rank = 0;
 #pragma unroll 16
-    for (int j = 0; j < groups; ++j) {
-      const uint64_t other = lds.group[j];
-      rank += other > mine || (other == mine && j < tid);
-    }
+    for (int j = 0; j < groups; ++j) rank += lds.group[j] > mine;
     if (rank == k - 1) lds.bound = mine;
   }
   __syncthreads();
@@ -261,14 +261,34 @@ __device__ __forceinline__ void emit_top(const LogprobArgs& g, int64_t row, int 
   g.top_logprobs[row * g.top + rank] = r.broken ? __builtin_nanf("") : r.log_p(key_value(key), g.scale);
 }
 
+// Where a block's part of a row is.  Rows in parts are few, so 32 bits do.
+template <typename T>
+struct Part {
+  int64_t row;
+  const T* z;
+  Cut<T> cut;
+  int v0, v1, edges;  // its vectors; the first part has the row's edges
+  template <typename Args>
+  __device__ Part(const Args& g, int64_t block)
+      : row(g.parts == 1 ? block : (unsigned)block / (unsigned)g.parts),
+        z(static_cast<const T*>(g.logits) + row * g.stride),
+        cut(z, g.vocab) {
+    const unsigned part = g.parts == 1 ? 0 : (unsigned)block - (unsigned)row * g.parts;
+    const unsigned each = ((unsigned)cut.nvec + g.parts - 1) / (unsigned)g.parts;
+    v0 = (int)(part * each < (unsigned)cut.nvec ? part * each : cut.nvec);
+    v1 = (int)((unsigned)v0 + each < (unsigned)cut.nvec ? v0 + each : cut.nvec);
+    edges = part == 0 ? cut.edges : 0;
+  }
+};
+
 // A block has one of a row's `parts`: all of it, and the results, or a stretch of its vectors, whose sums and
 // first keys go to the workspace for logprobs_join_kernel.
 //
 // For the alternatives a thread notes the largest of its elements, and in LDS the largest of each of kNotes
 // stretches of its vectors.  The stretches that reach the bound are listed, and all threads together read
 // their vectors again.  (Threads reading all of theirs again, 16 bytes of each line, cost as much as the
-// pass; threads reading their own stretches, one after the other, as much in latency.)  A single
-// wavefront's row is one batch, which is still in registers.
+// pass; threads reading their own stretches, one after the other, as much in latency.)  What was a single batch
+// is still in registers.
 constexpr int kNotes = 16, kItems = 1024;
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
@@ -280,18 +300,16 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
   __shared__ int items[NOTES ? kItems : 1];  // stretch * NT + thread
   const int64_t block = block_row();
   if (block >= g.rows * g.parts) return;
-  const int64_t row = g.parts == 1 ? block : block / g.parts;
-  const int part = g.parts == 1 ? 0 : (int)(block % g.parts);
-  const T* z = static_cast<const T*>(g.logits) + row * g.stride;
+  const Part<T> at(g, block);
+  const int64_t row = at.row;
+  const T* z = at.z;
   const Scale<false> k{g.scale * kLog2e};
-  const Cut<T> cut(z, g.vocab);
-  const int v0 = (int)((int64_t)cut.nvec * part / g.parts), v1 = (int)((int64_t)cut.nvec * (part + 1) / g.parts);
-  const int edges = part == 0 ? cut.edges : 0;
-  const bool has_edge = (int)threadIdx.x < edges;
+  const Cut<T>& cut = at.cut;
+  const int v0 = at.v0, v1 = at.v1;
+  const bool whole = g.parts == 1, has_edge = (int)threadIdx.x < at.edges;
   const int edge_at = has_edge ? cut.edge(threadIdx.x) : -1;
-  const float edge = has_edge ? (float)z[edge_at] : -__builtin_inff();
-  const int64_t token = g.logprob ? g.tokens[row] : -1;
-  const float z_token = token >= 0 && token < g.vocab ? (float)z[token] : 0.f;
+  const T edge_raw = z[has_edge ? edge_at : 0];  // converted, and so waited for, after the row
+  const int64_t token = whole && g.logprob ? g.tokens[row] : -1;
   Sums<false> o;
   float high = -__builtin_inff();  // the thread's largest, and where its vector (or edge element) starts
   int high_at = v0 + (int)threadIdx.x < v1 ? cut.start(v0 + threadIdx.x) : edge_at;
@@ -322,6 +340,8 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
       }
     }
   });
+  const float edge = has_edge ? (float)edge_raw : -__builtin_inff();
+  const T token_raw = z[token >= 0 && token < g.vocab ? token : 0];
   if (has_edge) {
     o.template one<true>(edge, k);
     if (TOP && (high_at < 0 || key_of(edge, edge_at) > key_of(high, high_at))) {  // it may stand before the vectors
@@ -346,9 +366,8 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
     r = row_sums(w);
     sums = make_float4(w.ref, w.s, w.a, 1.f);
   }
-  const bool whole = g.parts == 1;
   if (threadIdx.x == 0) {
-    if (whole) finish_logprobs(g, row, z_token, token, r);
+    if (whole) finish_logprobs(g, row, (float)token_raw, token, r);
     else g.part_sums[block] = sums;
   }
   if constexpr (TOP) {
@@ -362,7 +381,13 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
     const bool mine = best && best >= bound;
     bool complete = true;
     if (mine && has_edge && key_of(edge, edge_at) >= bound) top_push(top, key_of(edge, edge_at));
-    if constexpr (NOTES) {
+    if (!NOTES || batches <= 1) {  // the row is still in registers
+      if (mine) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (v0 + (int)threadIdx.x + u * NT < v1) search(x[u], cut.start(v0 + threadIdx.x + u * NT));
+      }
+    } else {
       if (mine) {
         const float least = bound ? key_value(bound) : -__builtin_inff();
         for (int n = 0; n < kNotes; ++n) {
@@ -381,10 +406,6 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
         const int v = v0 + item % NT + (item / NT * stretch + i % stretch) * NT;
         if (v < v1) search(widen<T>(load_packed(z + cut.start(v))), cut.start(v));
       }
-    } else if (mine) {
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-        if (v0 + (int)threadIdx.x + u * NT < v1) search(x[u], cut.start(v0 + threadIdx.x + u * NT));
     }
     top_finish<W>(
         g.top, top, complete,
@@ -404,7 +425,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
         },
         [&](int rank, uint64_t key) {
           if (whole) emit_top(g, row, rank, key, r);
-          else g.part_keys[block * g.top + rank] = key;
+          else g.part_keys[(row * g.top + rank) * g.parts + (block - row * g.parts)] = key;  // a thread of the join has several parts'
         });
   }
 }
@@ -425,20 +446,14 @@ __device__ __forceinline__ Sums<WIDE> join_parts(bool there, float4 sums, Scale<
 }
 
 // A row's results from its parts': every wavefront joins the sums, the block selects among the keys.
-__global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs g, int dtype) {
+template <typename T>
+__global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs g) {
   constexpr int NT = 64 * kWaves;
   __shared__ TopLds<kWaves> top;
   const int64_t row = block_row();
   if (row >= g.rows) return;
   const float c = g.scale * kLog2e;
   const int64_t token = g.logprob ? g.tokens[row] : -1;
-  float z_token = 0.f;
-  if (token >= 0 && token < g.vocab) {
-    const int64_t at = row * g.stride + token;
-    z_token = dtype == HVDX_FLOAT32   ? static_cast<const float*>(g.logits)[at]
-              : dtype == HVDX_FLOAT16 ? (float)static_cast<const _Float16*>(g.logits)[at]
-                                      : (float)static_cast<const __bf16*>(g.logits)[at];
-  }
   const uint64_t* keys = g.part_keys + row * g.parts * g.top;
   const int nkeys = g.parts * g.top, lane = threadIdx.x % 64;
   const bool there = lane < g.parts;
@@ -446,9 +461,10 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs 
   uint64_t best = 0;
   for (int i = threadIdx.x; i < nkeys; i += NT)
     if (keys[i] > best) best = keys[i];
+  const T z_token = static_cast<const T*>(g.logits)[row * g.stride + (token >= 0 && token < g.vocab ? token : 0)];
   const RowSums r = wide_row(there, sums, false) ? row_sums(join_parts<true>(there, sums, Scale<true>{c}))
                                                 : row_sums(join_parts<false>(there, sums, Scale<false>{c}));
-  if (threadIdx.x == 0) finish_logprobs(g, row, z_token, token, r);
+  if (threadIdx.x == 0) finish_logprobs(g, row, (float)z_token, token, r);
   if (!g.top) return;
   const uint64_t bound = top_bound<kWaves>(g.top, best, top);
   if (best && best >= bound)
@@ -467,6 +483,10 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs 
 
 // The gradients are element by element: a block has kChunk vectors of a row.
 constexpr int kChunkBatches = 2, kChunk = kChunkBatches * kBatch * 64 * kWaves;
+__device__ __forceinline__ int64_t row_of(int64_t block, int64_t chunks) {
+  if (chunks == 1) return block;
+  return block >> 32 ? block / chunks : (unsigned)block / (unsigned)chunks;  // a tenth of the 64-bit division's time
+}
 inline int64_t row_chunks(int64_t vocab, int n) {
   const int64_t chunks = (vocab / n + kChunk - 1) / kChunk;
   return chunks < 1 ? 1 : chunks;
@@ -498,7 +518,7 @@ template <typename T>
 __global__ __launch_bounds__(64 * kWaves) void logprobs_grad_kernel(LogprobGradArgs g) {
   const int64_t block = block_row();
   if (block >= g.rows * g.chunks) return;
-  const int64_t row = g.chunks == 1 ? block : block / g.chunks;
+  const int64_t row = row_of(block, g.chunks);
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
   const float c = g.scale * kLog2e;
@@ -868,15 +888,12 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs g, uint32_t
   __shared__ DistillStats shared;
   const int64_t block = block_row();
   if (block >= g.rows * g.parts) return;
-  const int64_t row = g.parts == 1 ? block : block / g.parts;
-  const int part = g.parts == 1 ? 0 : (int)(block % g.parts);
-  const T* z = static_cast<const T*>(g.logits) + row * g.stride;
-  const Cut<T> cut(z, g.vocab);
+  const Part<T> at(g, block);
+  const int64_t row = at.row;
+  const T* z = at.z;
+  const Cut<T>& cut = at.cut;
   const Scale<false> k{g.scale * kLog2e};
-  DistillBlock<T> b{row, block, 0, 0, z, cut, part == 0 && (int)threadIdx.x < cut.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts,
-                    &shared};
-  b.v0 = (int)((int64_t)cut.nvec * part / g.parts);
-  b.v1 = (int)((int64_t)cut.nvec * (part + 1) / g.parts);
+  DistillBlock<T> b{row, block, at.v0, at.v1, z, cut, (int)threadIdx.x < at.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts, &shared};
   b.edge_at = b.has_edge ? cut.edge(threadIdx.x) : 0;
   b.edge = b.has_edge ? (float)z[b.edge_at] : -__builtin_inff();
   if (threadIdx.x < 64 && (REST || g.parts == 1)) {
@@ -939,7 +956,7 @@ __global__ __launch_bounds__(64 * kWaves) void distill_grad_kernel(DistillArgs g
   constexpr int N = RowTypes<T>::n;
   const int64_t block = block_row();
   if (block >= g.rows * g.chunks) return;
-  const int64_t row = g.chunks == 1 ? block : block / g.chunks;
+  const int64_t row = row_of(block, g.chunks);
   const int chunk = (int)(block - row * g.chunks), lane = threadIdx.x % 64;
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   T* out = static_cast<T*>(g.grad) + row * g.grad_stride;
@@ -973,7 +990,14 @@ uint32_t bitmap_bytes(int64_t vocab, int n, bool rest) {
 
 }  // namespace
 
+// Few rows leave most of the chip idle.  A block of 1024 threads a row is the fastest for them (us for 200 rows of
+// 131072 bf16 with 20 alternatives: 18.5, split 25.3, 256 threads a row 32), but for long rows of very few,
+// which one compute unit takes longer over than it takes to join parts (24 rows of 131072: bf16 16.2, split
+// 15.7, binary32 17.6 and 14.9; one of 200000 binary32 23.0 and 13.8; 100 of them 25.3 and 27.5; one of 32768
+// 7.9 and 10.6).
+constexpr int64_t kFewRows = 256, kSplitRows = 48, kSplitVocab = 98304;
 int row_parts(int64_t rows, int64_t vocab) {
+  if (rows > kSplitRows || vocab < kSplitVocab) return 1;
   int64_t parts = (kBlocksWanted + rows - 1) / rows;
   if (parts > vocab / kPartLeast) parts = vocab / kPartLeast;
   return parts < 1 ? 1 : parts > kPartsMost ? kPartsMost : (int)parts;
@@ -986,6 +1010,9 @@ hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream) 
     if (g.vocab / RowTypes<T>::n <= 64 * kBatch) {  // one batch of one wavefront
       if (g.top) HVDX_LAUNCH((logprobs_kernel<T, 1, true>), grid, dim3(64), 0, stream, g);
       else HVDX_LAUNCH((logprobs_kernel<T, 1, false>), grid, dim3(64), 0, stream, g);
+    } else if (g.parts == 1 && g.rows <= kFewRows) {
+      if (g.top) HVDX_LAUNCH((logprobs_kernel<T, 16, true>), grid, dim3(1024), 0, stream, g);
+      else HVDX_LAUNCH((logprobs_kernel<T, 16, false>), grid, dim3(1024), 0, stream, g);
     } else {
       if (g.top) HVDX_LAUNCH((logprobs_kernel<T, kWaves, true>), grid, dim3(64 * kWaves), 0, stream, g);
       else HVDX_LAUNCH((logprobs_kernel<T, kWaves, false>), grid, dim3(64 * kWaves), 0, stream, g);
@@ -995,7 +1022,9 @@ hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream) 
 }
 
 hipError_t launch_logprobs_join(const LogprobArgs& g, int dtype, hipStream_t stream) {
-  HVDX_LAUNCH(logprobs_join_kernel, row_grid(g.rows), dim3(64 * kWaves), 0, stream, g, dtype);
+  by_type(dtype, [&](auto t) {
+    HVDX_LAUNCH(logprobs_join_kernel<decltype(t)>, row_grid(g.rows), dim3(64 * kWaves), 0, stream, g);
+  });
   return hipGetLastError();
 }
 
@@ -1035,8 +1064,11 @@ hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream) {
 #define HVDX_ROW(w, nv) row(integral_constant<int, w>{}, integral_constant<int, nv>{})
     if (g.parts > 1 || !g.grad || vectors < 2) {  // fewer may hold no vector on its boundary
       if (vectors <= 256) pass(integral_constant<int, 1>{});
+      else if (g.parts == 1 && g.rows <= kFewRows) pass(integral_constant<int, 16>{});
       else pass(integral_constant<int, kWaves>{});
     } else if (vectors <= 256) HVDX_ROW(1, 4);
+    else if (g.rows <= kFewRows && vectors <= 4096) HVDX_ROW(16, 4);
+    else if (g.rows <= kFewRows && vectors <= 8192) HVDX_ROW(16, 8);
     else if (vectors <= 1024) HVDX_ROW(4, 4);
     else if (vectors <= 2048) HVDX_ROW(4, 8);
     else if (vectors <= 4096) HVDX_ROW(8, 8);

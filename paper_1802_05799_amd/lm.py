@@ -26,22 +26,23 @@ from .cycle import current_stream
 _DTYPE = {torch.float32: L.FLOAT32, torch.float16: L.FLOAT16, torch.bfloat16: L.BFLOAT16}
 
 
-def _rows(name, x, length, most, device):
-    """Checks a matrix of rows; returns (rows, row stride)."""
-    if x.dim() != 2 or x.shape[1] != length or x.shape[0] > most:
-        raise ValueError(f"{name}: shape {tuple(x.shape)}, expected at most {most} rows of {length}")
-    if x.device != device:
-        raise ValueError(f"{name} is on {x.device}, expected {device}")
-    rows, stride = x.shape[0], x.stride()
-    if stride[1] != 1 and length > 1 or rows > 1 and stride[0] < length:
+def _rows(name, x, length, most, index):
+    """Checks a matrix of rows on GPU `index`; returns (rows, row stride)."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 2 or shape[1] != length or shape[0] > most:
+        raise ValueError(f"{name}: shape {tuple(shape)}, expected at most {most} rows of {length}")
+    if x.get_device() != index:
+        raise ValueError(f"{name} is on {x.device}, expected GPU {index}")
+    rows, apart = shape[0], stride[0]
+    if stride[1] != 1 and length > 1 or apart < length and rows > 1:
         raise ValueError(f"{name}: strides {stride}: a row's elements must lie side by side, and rows apart")
-    return rows, max(stride[0], length)
+    return rows, apart if apart > length else length
 
 
-def _like(name, x, shape, dtype, device):
-    """Checks a dense operand of fixed shape and type; returns its address."""
-    if x.shape != shape or x.dtype != dtype or x.device != device or not x.is_contiguous():
-        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)} on {x.device}, expected contiguous {dtype} {tuple(shape)} on {device}")
+def _like(name, x, shape, dtype, index):
+    """Checks a dense operand of fixed shape and type on GPU `index`; returns its address."""
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != index or not x.is_contiguous():
+        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)} on {x.device}, expected contiguous {dtype} {tuple(shape)} on GPU {index}")
     return x.data_ptr()
 
 
@@ -55,6 +56,7 @@ class _Operator:
     """Device, and the streams that the object's tensors are used on."""
 
     def _own(self, device, **tensors):
+        self._index = device.index
         self._tensors = [t for t in tensors.values() if t is not None and t.numel()]
         self._streams = {current_stream(device)}
         for name, t in tensors.items():
@@ -100,8 +102,8 @@ class TokenLogprobs(_Operator):
     def __call__(self, logits, tokens=None, scale: float = 1.0, stream: int | None = None) -> None:
         """tokens: int64 [rows], negative for none (log probability 0); without them `logprob` is left as it was."""
         dtype = _type("logits", logits.dtype)
-        rows, stride = _rows("logits", logits, self.vocab, self.rows, self.device)
-        at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self.device)
+        rows, stride = _rows("logits", logits, self.vocab, self.rows, self._index)
+        at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self._index)
         out = self._out if at else (0, *self._out[1:])
         L.hvdx_token_logprobs(logits.data_ptr(), stride, dtype, rows, self.vocab, scale, at, *out, self._stream(stream))
         self.scale = scale
@@ -112,10 +114,10 @@ class TokenLogprobs(_Operator):
         if self.scale is None:
             raise ValueError("grad before the first call")
         dtype = _type("logits", logits.dtype)
-        rows, stride = _rows("logits", logits, self.vocab, self.rows, self.device)
-        at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self.device)
-        a = 0 if grad_logprob is None else _like("grad_logprob", grad_logprob, (rows,), torch.float32, self.device)
-        b = 0 if grad_entropy is None else _like("grad_entropy", grad_entropy, (rows,), torch.float32, self.device)
+        rows, stride = _rows("logits", logits, self.vocab, self.rows, self._index)
+        at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self._index)
+        a = 0 if grad_logprob is None else _like("grad_logprob", grad_logprob, (rows,), torch.float32, self._index)
+        b = 0 if grad_entropy is None else _like("grad_entropy", grad_entropy, (rows,), torch.float32, self._index)
         out, out_stride = _grad_of(logits, out)
         L.hvdx_token_logprobs_grad(logits.data_ptr(), stride, dtype, rows, self.vocab, self.scale, at,
                                    self.stats.data_ptr(), a, b, out.data_ptr(), out_stride, self._stream(stream))
@@ -127,7 +129,7 @@ def _grad_of(logits, out):
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     elif out.dtype != logits.dtype or out.shape != logits.shape:
         raise ValueError(f"out: {out.dtype} {tuple(out.shape)}, expected {logits.dtype} {tuple(logits.shape)}")
-    return out, _rows("out", out, logits.shape[1], logits.shape[0], logits.device)[1]
+    return out, _rows("out", out, logits.shape[1], logits.shape[0], logits.get_device())[1]
 
 
 class DistillLoss(_Operator):
@@ -151,10 +153,10 @@ class DistillLoss(_Operator):
 
     def _inputs(self, logits, ids, logprobs):
         dtype = _type("logits", logits.dtype)
-        rows, stride = _rows("logits", logits, self.vocab, self.rows, self.device)
+        rows, stride = _rows("logits", logits, self.vocab, self.rows, self._index)
         shape = (rows, self.alternatives)
         return rows, (logits.data_ptr(), stride, dtype, rows, self.vocab), (
-            _like("ids", ids, shape, torch.int64, self.device), _like("logprobs", logprobs, shape, torch.float32, self.device),
+            _like("ids", ids, shape, torch.int64, self._index), _like("logprobs", logprobs, shape, torch.float32, self._index),
             self.alternatives, self.rest)
 
     def __call__(self, logits, ids, logprobs, scale: float = 1.0, grad_loss=None, out=None, stream: int | None = None) -> None:
@@ -165,7 +167,7 @@ class DistillLoss(_Operator):
             raise ValueError("grad_loss and out go together")
         g = at = out_stride = 0
         if out is not None:
-            g = _like("grad_loss", grad_loss, (rows,), torch.float32, self.device)
+            g = _like("grad_loss", grad_loss, (rows,), torch.float32, self._index)
             at, out_stride = out.data_ptr(), _grad_of(logits, out)[1]
         L.hvdx_distill(*head, scale, *teacher, g, self.loss.data_ptr(), self.stats.data_ptr(), at, out_stride,
                        self.workspace.data_ptr(), self._bytes, self._stream(stream))
@@ -176,7 +178,7 @@ class DistillLoss(_Operator):
         if self.scale is None:
             raise ValueError("grad before the first call")
         rows, head, teacher = self._inputs(logits, ids, logprobs)
-        g = _like("grad_loss", grad_loss, (rows,), torch.float32, self.device)
+        g = _like("grad_loss", grad_loss, (rows,), torch.float32, self._index)
         out, out_stride = _grad_of(logits, out)
         L.hvdx_distill_grad(*head, self.scale, *teacher, self.stats.data_ptr(), g, out.data_ptr(), out_stride,
                             self._stream(stream))
@@ -223,7 +225,7 @@ class ResidualNorm(_Operator):
     def _row_input(self, name, x):
         if x.dtype != self.dtype:
             raise ValueError(f"{name}: type {x.dtype}, expected {self.dtype}")
-        rows, stride = _rows(name, x, self.dim, self.rows, self.device)
+        rows, stride = _rows(name, x, self.dim, self.rows, self._index)
         if rows != self.rows:
             raise ValueError(f"{name}: {rows} rows, expected {self.rows}")
         return x.data_ptr(), stride
@@ -231,7 +233,7 @@ class ResidualNorm(_Operator):
     def _parameters(self, weight, post, gate):
         if (post is not None) != self.post or (gate is not None) != bool(self.gate_rows):
             raise ValueError("post_weight and gate must be given exactly if the object was built with them")
-        f32, shape, d = torch.float32, (self.dim,), self.device
+        f32, shape, d = torch.float32, (self.dim,), self._index
         return (0 if weight is None else _like("weight", weight, shape, f32, d), 0 if post is None else _like("post_weight", post, shape, f32, d),
                 0 if gate is None else _like("gate", gate if gate.dim() == 2 else gate.view(1, -1), self._gate, self.gate_dtype, d))
 
