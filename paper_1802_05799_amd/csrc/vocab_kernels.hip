@@ -747,11 +747,11 @@ __device__ __forceinline__ void distill_row_results(const DistillArgs& g, const 
 }
 
 // The sums over a row or a part, its logits from memory.
-template <int W, bool REST, bool WIDE, typename T>
+template <int W, bool REST, bool STREAM, bool WIDE, typename T>
 __device__ __forceinline__ Sums<WIDE> distill_sums(const DistillBlock<T>& b, Scale<WIDE> k, bool exact) {
   constexpr int NT = 64 * W, N = RowTypes<T>::n;
   Sums<WIDE> o;
-  for_batches<NT, false>(b.z, b.cut, b.v0, b.v1, [&](int i, const Packed<T>(&p)[kBatch]) {
+  for_batches<NT, STREAM>(b.z, b.cut, b.v0, b.v1, [&](int i, const Packed<T>(&p)[kBatch]) {
     Wide<T> x[kBatch];
     float hi = kNone;
 #pragma unroll
@@ -851,7 +851,7 @@ __global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g) {
   o = over_block<W>(o, k, parts);
   if (!plain(o.ref) || (REST && __builtin_amdgcn_readfirstlane(ids[64]))) {
     const Scale<true> kw{k.c};
-    const Sums<true> w = distill_sums<W, REST>(b, kw, true);
+    const Sums<true> w = distill_sums<W, REST, false>(b, kw, true);
     distill_row_results<REST>(g, b, w, kw);
     distill_write<W, REST>(g, b, w, kw);
     return;
@@ -877,9 +877,9 @@ __global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g) {
   if (threadIdx.x < 64) patch_listed(g, out, b.e, scaled, shared);
 }
 
-// The sums of one of a row's parts; with one part the row's loss and stats, and with `grad` its gradient, for which
-// the logits are read again (a row too long for registers: from the Infinity Cache).
-template <typename T, int W, bool REST>
+// The sums of one of a row's parts; with one part the row's loss and stats; GRAD: its gradient too, for which the
+// logits are read again (rows too long for registers, and those of less than two vectors).
+template <typename T, int W, bool REST, bool GRAD>
 __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs g, uint32_t mask) {
   constexpr int NT = 64 * W;
   extern __shared__ uint32_t words[];
@@ -908,19 +908,19 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs g, uint32_t
   const bool huge = REST && __builtin_amdgcn_readfirstlane(ids[64]);
   const bool exact = (uint32_t)cut.nvec <= mask + 1;
   auto rest = [&](auto o, auto by) {
-    if (g.parts > 1) {
+    if (!GRAD && g.parts > 1) {
       if (threadIdx.x == 0) g.part_sums[block] = make_float4(o.ref, o.s, 0.f, std::is_same_v<decltype(by), Scale<true>> ? 1.f : 0.f);
       return;
     }
     distill_row_results<REST>(g, b, o, by);
-    if (g.grad) distill_write<W, REST>(g, b, o, by);
+    if constexpr (GRAD) distill_write<W, REST>(g, b, o, by);
   };
-  const Sums<false> o = distill_sums<W, REST>(b, k, exact);
+  const Sums<false> o = distill_sums<W, REST, !GRAD>(b, k, exact);
   if (plain(o.ref) && !huge) {
     rest(o, k);
   } else {
     const Scale<true> kw{k.c};
-    rest(distill_sums<W, REST>(b, kw, exact), kw);
+    rest(distill_sums<W, REST, !GRAD>(b, kw, exact), kw);
   }
 }
 
@@ -1048,11 +1048,12 @@ hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream) {
     using T = decltype(t);
     const int64_t vectors = g.vocab / RowTypes<T>::n;
     const uint32_t bytes = bitmap_bytes(g.vocab, RowTypes<T>::n, g.rest);
-    auto pass = [&](auto w) {
+    auto pass = [&](auto w, auto grad) {
       constexpr int W = w();
+      constexpr bool GRAD = grad();
       const dim3 grid = row_grid(g.rows * g.parts), threads(64 * W);
-      if (g.rest) HVDX_LAUNCH((distill_kernel<T, W, true>), grid, threads, bytes, stream, g, bytes - 1);
-      else HVDX_LAUNCH((distill_kernel<T, W, false>), grid, threads, bytes, stream, g, bytes - 1);
+      if (g.rest) HVDX_LAUNCH((distill_kernel<T, W, true, GRAD>), grid, threads, bytes, stream, g, bytes - 1);
+      else HVDX_LAUNCH((distill_kernel<T, W, false, GRAD>), grid, threads, bytes, stream, g, bytes - 1);
     };
     auto row = [&](auto w, auto nv) {
       constexpr int W = w(), NV = nv();
@@ -1062,10 +1063,14 @@ hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream) {
     };
     using std::integral_constant;
 #define HVDX_ROW(w, nv) row(integral_constant<int, w>{}, integral_constant<int, nv>{})
-    if (g.parts > 1 || !g.grad || vectors < 2) {  // fewer may hold no vector on its boundary
-      if (vectors <= 256) pass(integral_constant<int, 1>{});
-      else if (g.parts == 1 && g.rows <= kFewRows) pass(integral_constant<int, 16>{});
-      else pass(integral_constant<int, kWaves>{});
+    using std::false_type;
+    using std::true_type;
+    if (g.parts > 1 || !g.grad) {
+      if (vectors <= 256) pass(integral_constant<int, 1>{}, false_type{});
+      else if (g.parts == 1 && g.rows <= kFewRows) pass(integral_constant<int, 16>{}, false_type{});
+      else pass(integral_constant<int, kWaves>{}, false_type{});
+    } else if (vectors < 2) {  // there may be no vector on its boundary
+      pass(integral_constant<int, 1>{}, true_type{});
     } else if (vectors <= 256) HVDX_ROW(1, 4);
     else if (g.rows <= kFewRows && vectors <= 4096) HVDX_ROW(16, 4);
     else if (g.rows <= kFewRows && vectors <= 8192) HVDX_ROW(16, 8);
@@ -1074,7 +1079,7 @@ hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream) {
     else if (vectors <= 4096) HVDX_ROW(8, 8);
     else if (vectors <= 8192) HVDX_ROW(8, 16);
     else if (vectors <= kRowMost) HVDX_ROW(16, 16);
-    else pass(integral_constant<int, 16>{});
+    else pass(integral_constant<int, 16>{}, true_type{});
 #undef HVDX_ROW
   });
   return hipGetLastError();
