@@ -574,7 +574,7 @@ int hvdx_fold_allreduce(void* const* bufs, int nranks, int64_t count, int dtype,
  *
  * hvdx_token_logprobs -- for each row z of `vocab` logits, with p = softmax(scale z): the log probability of
  * one token, the entropy -sum p log p, and the `top` likeliest tokens with their log probabilities.
- *   scale          one over the temperature; > 0, finite
+ *   scale          one over the temperature, 1e-30 .. 1e30
  *   tokens[rows]   a token < 0 is none (its log probability is 0), one >= vocab gives NaN; NULL with logprob
  *   logprob, entropy [rows]  float, out; NULL where not wanted
  *   top            0 .. HVDX_MAX_TOP, at most vocab

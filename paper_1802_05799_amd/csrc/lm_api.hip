@@ -35,6 +35,7 @@ Buffer vec(const char* name, const void* p, int64_t count, int size, int align =
   return {name, p, count * size, 0, align ? align : size};
 }
 Buffer matrix(const char* name, const void* p, int64_t rows, int64_t length, int64_t stride, int size) {
+  if (rows == 1) stride = length;  // whatever was given
   return {name, p, ((rows - 1) * stride + length) * size, stride * size, size};
 }
 
@@ -84,7 +85,7 @@ int check_stride(const char* name, int64_t stride, int64_t length, int64_t rows,
 }
 
 int check_scale(float scale, const char* what) {
-  return scale > 0.f && isfinite(scale) ? HVDX_OK : fail(HVDX_ERR_INVALID, "%s: scale %g is not positive and finite", what, scale);
+  return scale >= 1e-30f && scale <= 1e30f ? HVDX_OK : fail(HVDX_ERR_INVALID, "%s: scale %g outside 1e-30..1e30", what, scale);
 }
 
 int check_workspace(const void* workspace, size_t given, size_t need, const char* what) {
@@ -279,7 +280,7 @@ int hvdx_residual_norm(const void* x, int64_t x_stride, const void* y, int64_t y
   if (!x_out && !h_out && !stats) return fail(HVDX_ERR_INVALID, "%s: no output", what);
   if (!y && x_out) return fail(HVDX_ERR_INVALID, "%s: x_out without y", what);
   const int es = row_elem_size(dtype), gs = gate && gate_dtype == HVDX_FLOAT32 ? 4 : es;
-  const Buffer in[] = {matrix("x", x, rows, dim, rows > 1 ? x_stride : dim, es), matrix("y", y, rows, dim, rows > 1 ? y_stride : dim, es),
+  const Buffer in[] = {matrix("x", x, rows, dim, x_stride, es), matrix("y", y, rows, dim, y_stride, es),
                        vec("post", post, dim, 4), vec("gate", gate, gate ? rows / gate_rows * dim : 0, gs),
                        vec("weight", weight, dim, 4)};
   const Buffer out[] = {matrix("x_out", x_out, rows, dim, dim, es), matrix("h_out", h_out, rows, dim, dim, es),
@@ -322,7 +323,7 @@ int hvdx_residual_norm_grad(const void* x, int64_t x_stride, const void* y, int6
   const int es = row_elem_size(dtype), gs = gate && gate_dtype == HVDX_FLOAT32 ? 4 : es;
   const int64_t gates = gate ? rows / gate_rows * dim : 0;
   const auto rows_of = [&](const char* name, const void* p, int64_t stride) {
-    return matrix(name, p, rows, dim, rows > 1 ? stride : dim, es);
+    return matrix(name, p, rows, dim, stride, es);
   };
   const Buffer in[] = {rows_of("x", x, x_stride), rows_of("y", y, y_stride), rows_of("dx", dx, dx_stride),
                        rows_of("dh", dh, dh_stride), vec("post", post, dim, 4), vec("gate", gate, gates, gs),

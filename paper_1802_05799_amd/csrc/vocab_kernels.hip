@@ -291,7 +291,7 @@ struct Part {
 // is still in registers.
 constexpr int kNotes = 16, kItems = 1024;
 template <typename T, int W, bool TOP>
-__global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
+__global__ __launch_bounds__(64 * W, TOP ? 6 : 1) void logprobs_kernel(LogprobArgs g) {
   constexpr int NT = 64 * W, N = RowTypes<T>::n;
   constexpr bool NOTES = TOP && W > 1;
   __shared__ float parts[W][3];
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(64 * W) void logprobs_kernel(LogprobArgs g) {
     const bool mine = best && best >= bound;
     bool complete = true;
     if (mine && has_edge && key_of(edge, edge_at) >= bound) top_push(top, key_of(edge, edge_at));
-    if (!NOTES || batches <= 1) {  // the row is still in registers
+    if (!NOTES || batches <= 1) {
       if (mine) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
@@ -849,7 +849,8 @@ __global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g) {
   if (b.has_edge && !b.edge_listed) o.template one<false>(b.edge, k);
   note_huge<REST>(b.e, k.c, ids);
   o = over_block<W>(o, k, parts);
-  if (!plain(o.ref) || (REST && __builtin_amdgcn_readfirstlane(ids[64]))) {
+  // (a single wavefront has no barrier between the note and its reading)
+  if (!plain(o.ref) || (REST && (W == 1 ? __any(huge_entry(b.e, k.c)) : __builtin_amdgcn_readfirstlane(ids[64])))) {
     const Scale<true> kw{k.c};
     const Sums<true> w = distill_sums<W, REST, false>(b, kw, true);
     distill_row_results<REST>(g, b, w, kw);
@@ -1006,17 +1007,16 @@ int row_parts(int64_t rows, int64_t vocab) {
 hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream) {
   by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    const dim3 grid = row_grid(g.rows * g.parts);
-    if (g.vocab / RowTypes<T>::n <= 64 * kBatch) {  // one batch of one wavefront
-      if (g.top) HVDX_LAUNCH((logprobs_kernel<T, 1, true>), grid, dim3(64), 0, stream, g);
-      else HVDX_LAUNCH((logprobs_kernel<T, 1, false>), grid, dim3(64), 0, stream, g);
-    } else if (g.parts == 1 && g.rows <= kFewRows) {
-      if (g.top) HVDX_LAUNCH((logprobs_kernel<T, 16, true>), grid, dim3(1024), 0, stream, g);
-      else HVDX_LAUNCH((logprobs_kernel<T, 16, false>), grid, dim3(1024), 0, stream, g);
-    } else {
-      if (g.top) HVDX_LAUNCH((logprobs_kernel<T, kWaves, true>), grid, dim3(64 * kWaves), 0, stream, g);
-      else HVDX_LAUNCH((logprobs_kernel<T, kWaves, false>), grid, dim3(64 * kWaves), 0, stream, g);
-    }
+    using std::integral_constant;
+    auto run = [&](auto w) {
+      constexpr int W = w();
+      const dim3 grid = row_grid(g.rows * g.parts), threads(64 * W);
+      if (g.top) HVDX_LAUNCH((logprobs_kernel<T, W, true>), grid, threads, 0, stream, g);
+      else HVDX_LAUNCH((logprobs_kernel<T, W, false>), grid, threads, 0, stream, g);
+    };
+    if (g.vocab / RowTypes<T>::n <= kBatch * 64) run(integral_constant<int, 1>{});  // one batch of one wavefront
+    else if (g.parts == 1 && g.rows <= kFewRows) run(integral_constant<int, 16>{});
+    else run(integral_constant<int, kWaves>{});
   });
   return hipGetLastError();
 }

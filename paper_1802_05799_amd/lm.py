@@ -62,6 +62,10 @@ class _Operator:
         for name, t in tensors.items():
             setattr(self, name, t)
 
+    def _of_last(self, rows):
+        if rows != self._last:
+            raise ValueError(f"a gradient of {rows} rows after a call of {self._last}")
+
     def _stream(self, stream):
         if stream is None:
             stream = current_stream(self.device)
@@ -97,7 +101,7 @@ class TokenLogprobs(_Operator):
                   top_logprobs=new(rows, top), stats=new(rows, 4), workspace=new(self._bytes, dtype=torch.uint8))
         self._out = (self.logprob.data_ptr(), self.entropy.data_ptr(), top, self.top_ids.data_ptr(),
                      self.top_logprobs.data_ptr(), self.stats.data_ptr(), self.workspace.data_ptr(), self._bytes)
-        self.scale = None  # the last call's
+        self.scale = self._last = None  # the last call's scale and rows
 
     def __call__(self, logits, tokens=None, scale: float = 1.0, stream: int | None = None) -> None:
         """tokens: int64 [rows], negative for none (log probability 0); without them `logprob` is left as it was."""
@@ -106,15 +110,14 @@ class TokenLogprobs(_Operator):
         at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self._index)
         out = self._out if at else (0, *self._out[1:])
         L.hvdx_token_logprobs(logits.data_ptr(), stride, dtype, rows, self.vocab, scale, at, *out, self._stream(stream))
-        self.scale = scale
+        self.scale, self._last = scale, rows
 
     def grad(self, logits, tokens, grad_logprob, grad_entropy=None, out=None, stream: int | None = None):
         """The logits' gradient for the last call's `logprob` and `entropy` (grad_logprob, grad_entropy: float32
         [rows], None for none) into `out` (of the logits' type; may be `logits`; None: a new tensor), which is returned."""
-        if self.scale is None:
-            raise ValueError("grad before the first call")
         dtype = _type("logits", logits.dtype)
         rows, stride = _rows("logits", logits, self.vocab, self.rows, self._index)
+        self._of_last(rows)
         at = 0 if tokens is None else _like("tokens", tokens, (rows,), torch.int64, self._index)
         a = 0 if grad_logprob is None else _like("grad_logprob", grad_logprob, (rows,), torch.float32, self._index)
         b = 0 if grad_entropy is None else _like("grad_entropy", grad_entropy, (rows,), torch.float32, self._index)
@@ -149,7 +152,7 @@ class DistillLoss(_Operator):
         self._bytes = L.hvdx_distill_workspace_bytes(rows, vocab)
         self._own(self.device, loss=torch.empty(rows, device=self.device), stats=torch.empty(rows, 8, device=self.device),
                   workspace=torch.empty(self._bytes, dtype=torch.uint8, device=self.device))
-        self.scale = None  # the last call's
+        self.scale = self._last = None  # the last call's scale and rows
 
     def _inputs(self, logits, ids, logprobs):
         dtype = _type("logits", logits.dtype)
@@ -171,13 +174,12 @@ class DistillLoss(_Operator):
             at, out_stride = out.data_ptr(), _grad_of(logits, out)[1]
         L.hvdx_distill(*head, scale, *teacher, g, self.loss.data_ptr(), self.stats.data_ptr(), at, out_stride,
                        self.workspace.data_ptr(), self._bytes, self._stream(stream))
-        self.scale = scale
+        self.scale, self._last = scale, rows
 
     def grad(self, logits, ids, logprobs, grad_loss, out=None, stream: int | None = None):
         """The logits' gradient for the last call's `loss`, into `out` (may be `logits`; None: a new tensor)."""
-        if self.scale is None:
-            raise ValueError("grad before the first call")
         rows, head, teacher = self._inputs(logits, ids, logprobs)
+        self._of_last(rows)
         g = _like("grad_loss", grad_loss, (rows,), torch.float32, self._index)
         out, out_stride = _grad_of(logits, out)
         L.hvdx_distill_grad(*head, self.scale, *teacher, self.stats.data_ptr(), g, out.data_ptr(), out_stride,
