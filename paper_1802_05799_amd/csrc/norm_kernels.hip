@@ -249,7 +249,8 @@ __global__ __launch_bounds__(64 * W * S) void norm_grad_kernel(NormGradArgs g) {
       for (int i = 0; i < NV; ++i) {
         if constexpr (!HELD) weights(i);
         if (!HELD || in_group == 0) gates(i, group);
-        const Floats<N> a = __builtin_convertvector(now.x[i], Floats<N>) * now.r.y, dh = __builtin_convertvector(now.dh[i], Floats<N>);
+        const Floats<N> a = __builtin_convertvector(now.x[i], Floats<N>) * now.r.y;
+        const Floats<N> dh = __builtin_convertvector(now.dh[i], Floats<N>);
         total(0, i) += dh * a;
         const Floats<N> b = dh * weight[i];
         sums[0] = dot<N>(a, b, sums[0], me.again[i]);
@@ -272,7 +273,8 @@ __global__ __launch_bounds__(64 * W * S) void norm_grad_kernel(NormGradArgs g) {
         gates(i, group);
       }
       const Floats<N> a = __builtin_convertvector(now.x[i], Floats<N>) * now.r.y;
-      Floats<N> d = __builtin_convertvector(now.dx[i], Floats<N>) + now.r.y * (__builtin_convertvector(now.dh[i], Floats<N>) * weight[i]);
+      const Floats<N> dh = __builtin_convertvector(now.dh[i], Floats<N>);
+      Floats<N> d = __builtin_convertvector(now.dx[i], Floats<N>) + now.r.y * (dh * weight[i]);
       d -= inner * a;
       if (g.grad_x && me.has(i)) stream_out<N>(static_cast<T*>(g.grad_x) + row * g.dim + me.at[i], d);
       if (!g.y) continue;

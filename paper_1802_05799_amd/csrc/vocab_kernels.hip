@@ -35,10 +35,7 @@ struct Cut {
     edges = vocab - nvec * n;
   }
   __device__ int start(int vec) const { return head + vec * n; }
-  __device__ const Packed<T>* of(const T* row, int first) const {
-    return reinterpret_cast<const Packed<T>*>(row + head) + first;
-  }
-  __device__ T* of(T* row, int first) const { return row + head + first * n + threadIdx.x * n; }
+  __device__ T* of(T* row, int first) const { return row + head + first * n + threadIdx.x * n; }  // the thread's from there
   __device__ int edge(int i) const { return i < head ? i : nvec * n + i; }  // 0 <= i < edges
 };
 
@@ -425,7 +422,7 @@ __global__ __launch_bounds__(64 * W, TOP ? 6 : 1) void logprobs_kernel(LogprobAr
         },
         [&](int rank, uint64_t key) {
           if (whole) emit_top(g, row, rank, key, r);
-          else g.part_keys[(row * g.top + rank) * g.parts + (block - row * g.parts)] = key;  // a thread of the join has several parts'
+          else g.part_keys[(row * g.top + rank) * g.parts + (block - row * g.parts)] = key;
         });
   }
 }
@@ -804,7 +801,8 @@ __global__ __launch_bounds__(64 * W, 4) void distill_row_kernel(DistillArgs g) {
   const T* z = static_cast<const T*>(g.logits) + row * g.stride;
   const Cut<T> cut(z, g.vocab);
   const Scale<false> k{g.scale * kLog2e};
-  DistillBlock<T> b{row, row, 0, cut.nvec, z, cut, (int)threadIdx.x < cut.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts, &shared};
+  DistillBlock<T> b{row,   row, 0,   cut.nvec, z,       cut,      (int)threadIdx.x < cut.edges, false,
+                    false, 0,   0.f, Entry{},  Listed{}, parts, &shared};
   // what is needed first is loaded before the row, behind which it would wait, and without a branch, at whose end
   // it would be waited for
   LoadedEntry in{};
@@ -894,7 +892,8 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs g, uint32_t
   const T* z = at.z;
   const Cut<T>& cut = at.cut;
   const Scale<false> k{g.scale * kLog2e};
-  DistillBlock<T> b{row, block, at.v0, at.v1, z, cut, (int)threadIdx.x < at.edges, false, false, 0, 0.f, Entry{}, Listed{}, parts, &shared};
+  DistillBlock<T> b{row,   block, at.v0, at.v1,   z,        cut,   (int)threadIdx.x < at.edges, false,
+                    false, 0,     0.f,   Entry{}, Listed{}, parts, &shared};
   b.edge_at = b.has_edge ? cut.edge(threadIdx.x) : 0;
   b.edge = b.has_edge ? (float)z[b.edge_at] : -__builtin_inff();
   if (threadIdx.x < 64 && (REST || g.parts == 1)) {
@@ -910,7 +909,8 @@ __global__ __launch_bounds__(64 * W) void distill_kernel(DistillArgs g, uint32_t
   const bool exact = (uint32_t)cut.nvec <= mask + 1;
   auto rest = [&](auto o, auto by) {
     if (!GRAD && g.parts > 1) {
-      if (threadIdx.x == 0) g.part_sums[block] = make_float4(o.ref, o.s, 0.f, std::is_same_v<decltype(by), Scale<true>> ? 1.f : 0.f);
+      constexpr bool WIDE = std::is_same_v<decltype(by), Scale<true>>;
+      if (threadIdx.x == 0) g.part_sums[block] = make_float4(o.ref, o.s, 0.f, WIDE ? 1.f : 0.f);
       return;
     }
     distill_row_results<REST>(g, b, o, by);

@@ -236,6 +236,32 @@ def test_in_place_through_the_abi(dtype):
     assert bool((c[-64:] == SENTINEL).all()) and bool((d[-64:] == SENTINEL).all())
 
 
+def test_objects_refuse():
+    x, w = torch.zeros(6, 64, device="cuda"), torch.ones(64, device="cuda")
+    gate = torch.ones(2, 64, device="cuda")
+    call = hv.ResidualNorm(6, 64, torch.float32, gate_rows=3)
+    for bad in (x[:5], x.half(), x.cpu(), x[:, :63], x.t().contiguous().t()):
+        with pytest.raises(ValueError):
+            call(bad, x, w, w, gate)
+        with pytest.raises(ValueError):
+            call(x, bad, w, w, gate)
+    for bad in ((w, None, gate), (w, w, None), (w[:5], w, gate), (w.half(), w, gate), (w, w, gate[:1]), (w, w, gate.half())):
+        with pytest.raises(ValueError):
+            call(x, x, *bad)
+    with pytest.raises(ValueError, match="y must be given"):
+        call(x, None, w, w, gate)
+    with pytest.raises(ValueError, match="grad=True"):
+        call.grad(x, x, x, w, w, gate)
+    call = hv.ResidualNorm(6, 64, torch.float32, block=False, grad=True)
+    with pytest.raises(ValueError, match="first call"):
+        call.grad(None, None, x, w)
+    call(x, None, w)
+    with pytest.raises(hv.HvdxError, match="dx and dh"):
+        call.grad(None, None, None, w)
+    with pytest.raises(ValueError, match="gate_dtype"):
+        hv.ResidualNorm(6, 64, torch.bfloat16, gate_rows=3, gate_dtype=torch.float16)
+
+
 def test_offsets_past_32_bits():
     """More than 2^31 elements: the last rows as if they were alone."""
     dim, rows = 16384, (1 << 17) + 40  # 2^31 + 655,360 elements

@@ -281,6 +281,38 @@ def test_distill_sizes(rows, vocab, dtype):
         check_distill(z, ids, t, 0.9, rest, f"rows {rows}")
 
 
+@pytest.mark.parametrize("rows,vocab,dtype", [(60, 140001, torch.float32), (50, 300007, torch.bfloat16), (7, 300007, torch.float16),
+                                              (2, 10, torch.bfloat16), (70, 17, torch.float32)])
+def test_distill_rows_read_twice(rows, vocab, dtype):
+    """Rows too long for registers (whose bitmap has fewer bytes than they have vectors), and of less than a vector or two."""
+    z = logits(rows, vocab, dtype, rows, offset=1)
+    if rows >= 16:
+        special_rows(z)
+    for rest in (True, False):
+        ids, t = alternatives(rows, vocab, 33, rows)
+        ids[:, 2] = vocab // 2
+        ids[:, 3] = min(vocab - 1, vocab // 2 + 16384 * 8)  # the same byte of a smaller bitmap
+        check_distill(z, ids, t, 1.1, rest, f"twice {vocab}", in_place=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_long_vocabulary(dtype):
+    """Positions that binary32 does not hold exactly."""
+    rows, vocab = 2, 40_000_003
+    z = logits(rows, vocab, dtype, 6)
+    tokens = torch.tensor([vocab - 1, 33_554_433], device="cuda")
+    z[0, vocab - 1] = 30.0
+    z[1, 33_554_433] = 30.0
+    call, _ = check_logprobs(z, tokens, 1.0, 16, "long")
+    a, b = torch.ones(rows, device="cuda"), torch.full((rows,), 0.1, device="cuda")
+    out = call.grad(z, tokens, a, b)
+    want = R.logprobs_grad(z, tokens, 1.0, a.double(), b.double())
+    R.assert_close(out, want, grad_bound(z, want, 1.0, a.double(), b.double(), vocab), dtype, "long grad")
+    del want, out
+    ids, t = torch.tensor([[vocab - 1, 5], [33_554_433, 33_554_432]], device="cuda"), torch.tensor([[-0.5, -2.0]] * rows, device="cuda")
+    check_distill(z, ids, t, 1.0, True, "long")
+
+
 def test_distill_peaked_student():
     """The listed tokens hold all but 1e-3 .. 1e-60 of the student's probability: the unlisted mass must not come from a
     difference."""
@@ -370,6 +402,42 @@ def test_fewer_rows_than_built_for():
     call(z[:0], tokens[:0])  # no rows: nothing happens
     call(z[5:6], tokens[5:6])
     assert torch.allclose(call.logprob[0], R.logprobs(z[5:6], tokens[5:6], 1.0, 0)["logprob"][0].float(), atol=1e-5)
+
+
+def test_objects_refuse():
+    call, ds = hv.TokenLogprobs(4, 100, top=2), hv.DistillLoss(4, 100, 3)
+    z, tokens = torch.zeros(4, 100, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    ids, t = torch.zeros(4, 3, dtype=torch.int64, device="cuda"), torch.zeros(4, 3, device="cuda")
+    g = torch.ones(4, device="cuda")
+    for bad in (z.double(), z.cpu(), z[:, :99], torch.zeros(5, 100, device="cuda"), z.t().contiguous().t(), z[:1].expand(4, 100), z[0]):
+        with pytest.raises(ValueError):
+            call(bad, tokens)
+        with pytest.raises(ValueError):
+            ds(bad, ids, t)
+    for bad in (tokens[:3], tokens.int(), tokens.cpu(), torch.zeros(8, dtype=torch.int64, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            call(z, bad)
+    with pytest.raises(hv.HvdxError, match="scale"):
+        call(z, tokens, scale=0.0)
+    with pytest.raises(hv.HvdxError, match="scale"):
+        call(z, tokens, scale=2e30)
+    with pytest.raises(ValueError, match="rows after"):
+        call.grad(z, tokens, g)  # before any call
+    call(z, tokens)
+    with pytest.raises(ValueError, match="rows after"):
+        call.grad(z[:2], tokens[:2], g[:2])
+    with pytest.raises(ValueError, match="out"):
+        call.grad(z, tokens, g, out=z.half())
+    with pytest.raises(hv.HvdxError, match="overlaps"):
+        wide = torch.zeros(4, 101, device="cuda")
+        call(wide[:, :100], tokens)
+        call.grad(wide[:, :100], tokens, g, out=wide[:, 1:])
+    with pytest.raises(ValueError, match="go together"):
+        ds(z, ids, t, grad_loss=g)
+    with pytest.raises(ValueError, match="ids"):
+        ds(z, ids[:, :2], t)
+    with pytest.raises(ValueError, match="logprobs"):
+        ds(z, ids, t.half())
 
 
 def test_another_stream():
