@@ -111,18 +111,23 @@ __device__ __forceinline__ void slot_sums(float (&x)[K], float (*lds)[K], int wa
   }
 }
 
-template <typename T, int N, int W, int NV, int S>
+// HELD: the weights stay in registers from row to row; rows of more than 16 elements a thread leave no room for
+// them, and take them from the caches.
+template <typename T, int N, int W, int NV, int S, bool HELD>
 __global__ __launch_bounds__(64 * W * S) void norm_kernel(NormArgs g) {
   __shared__ float lds[2][S][W][1];
   const Place<N, W, NV, S> me(g.dim);
   const float mean = 1.f / (float)g.dim;
   Floats<N> weight[NV], post[NV], gate[NV];
+  auto vector = [&](const float* p, int i) {
+    Floats<N> v = 1.f;
+    if (p && me.has(i)) v = load_elems<N>(p + me.at[i]);
+    return v;
+  };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    weight[i] = post[i] = gate[i] = 1.f;
-    if (!me.has(i)) continue;
-    if (g.weight) weight[i] = load_elems<N>(g.weight + me.at[i]);
-    if (g.post) post[i] = load_elems<N>(g.post + me.at[i]);
+    gate[i] = 1.f;
+    if constexpr (HELD) weight[i] = vector(g.weight, i), post[i] = vector(g.post, i);
   }
   int64_t group = -1;
   int turn = 0;
@@ -142,7 +147,7 @@ __global__ __launch_bounds__(64 * W * S) void norm_kernel(NormArgs g) {
       group = row / g.gate_rows;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
-        if (me.has(i)) gate[i] = load_gate<N, T>(g.gate, g.gate_f32, group * g.dim, me.at[i]);
+        if (HELD && me.has(i)) gate[i] = load_gate<N, T>(g.gate, g.gate_f32, group * g.dim, me.at[i]);
     }
     float ry = 1.f;
     if (g.post) {
@@ -154,6 +159,10 @@ __global__ __launch_bounds__(64 * W * S) void norm_kernel(NormArgs g) {
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      if constexpr (!HELD) {
+        post[i] = vector(g.post, i);
+        if (there && g.gate && me.has(i)) gate[i] = load_gate<N, T>(g.gate, g.gate_f32, group * g.dim, me.at[i]);
+      }
       v[i] += g.scale * (u[i] * (ry * post[i]) * gate[i]);
       sum[0] = dot<N>(v[i], v[i], sum[0], me.again[i]);
     }
@@ -163,6 +172,7 @@ __global__ __launch_bounds__(64 * W * S) void norm_kernel(NormArgs g) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (!me.has(i)) continue;
+      if constexpr (!HELD) weight[i] = vector(g.weight, i);
       if (g.x_out) stream_out<N>(static_cast<T*>(g.x_out) + row * g.dim + me.at[i], v[i]);
       if (g.h_out) stream_out<N>(static_cast<T*>(g.h_out) + row * g.dim + me.at[i], v[i] * rx * weight[i]);
     }
@@ -390,7 +400,7 @@ hipError_t launch_norm(const NormArgs& args, int dtype, hipStream_t stream) {
       const int64_t most = 256 * (32 / (W * S));
       if (blocks > most) blocks = most;
       g.row_step = blocks * S;
-      HVDX_LAUNCH((norm_kernel<T, n(), W, nv(), S>), row_grid(blocks), dim3(64 * W * S), 0, stream, g);
+      HVDX_LAUNCH((norm_kernel<T, n(), W, nv(), S, (n() * nv() <= 16)>), row_grid(blocks), dim3(64 * W * S), 0, stream, g);
     });
   });
   return hipGetLastError();

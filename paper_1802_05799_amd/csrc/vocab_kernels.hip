@@ -288,7 +288,7 @@ struct Part {
 // is still in registers.
 constexpr int kNotes = 16, kItems = 1024;
 template <typename T, int W, bool TOP>
-__global__ __launch_bounds__(64 * W, TOP ? 6 : 1) void logprobs_kernel(LogprobArgs g) {
+__global__ __launch_bounds__(64 * W, TOP && W < 16 ? 6 : 1) void logprobs_kernel(LogprobArgs g) {
   constexpr int NT = 64 * W, N = RowTypes<T>::n;
   constexpr bool NOTES = TOP && W > 1;
   __shared__ float parts[W][3];
