@@ -158,14 +158,20 @@ constexpr int kWaves = 4;
 // keys where they lie at random, so G is some four times k.  The threads collect those into LDS, where each
 // finds its rank by counting.  Where more reach it than LDS holds, k rounds over all keys find them one
 // by one.
-constexpr int kCandidates = 512;
+//
+// The bound is found by counting too, each of G threads going over all G; `halved`: by trying values, a wavefront
+// counting who reaches one by ballots.  That is less work for longer (some 2 us against 1), so it is for blocks of which
+// many share a compute unit and G = 256 (us for rows of bf16 with 64: 8192 x 8000 64 and counted 90, 1024 x 8000 13.9
+// and 18.9; one of 32768 with 8 10.4 and 7.8).  A single wavefront has G = 64 and so a useful bound for kTopShort keys
+// at most (8192 x 2000 with 64: 256 threads a row 50, one wavefront, by rounds, 180).
+constexpr int kCandidates = 512, kTopShort = 32;
 template <int W>
 struct TopLds {
   uint64_t group[64 * W], candidate[kCandidates], best[W], bound;
   int count, items;
 };
 template <int W>
-__device__ __forceinline__ uint64_t top_bound(int k, uint64_t best, TopLds<W>& lds) {  // ends with a barrier
+__device__ __forceinline__ uint64_t top_bound(int k, uint64_t best, TopLds<W>& lds, bool halved) {  // ends with a barrier
   const int tid = threadIdx.x;
   int groups = 64, span = W;  // groups of `span` threads
   while (span > 1 && groups < 4 * k) groups *= 2, span /= 2;
@@ -180,7 +186,36 @@ __device__ __forceinline__ uint64_t top_bound(int k, uint64_t best, TopLds<W>& l
     lds.bound = 0;  // where fewer than k groups have any: keys differ, but for the 0 of those that have none
   }
   __syncthreads();
-  if (tid < groups) {
+  if (W == kWaves && halved) {
+    if (tid < 64) {
+      uint64_t key[kWaves];
+#pragma unroll
+      for (int j = 0; j < kWaves; ++j) key[j] = tid + 64 * j < groups ? lds.group[tid + 64 * j] : 0;
+      // the first tried that k to `most` of them reach, between `high`, which fewer do, and `low`
+      const int most = k + k / 8;
+      int count = 0;
+      auto halve = [&](auto reaches) {
+        uint32_t low = 0, high = ~0u;
+        while (high - low > 1) {
+          const uint32_t mid = low + (high - low) / 2;
+          int n = 0;
+#pragma unroll
+          for (int j = 0; j < kWaves; ++j) n += __popcll(__ballot(reaches(key[j], mid)));
+          if (n < k) {
+            high = mid;
+          } else {
+            low = mid;
+            count = n;
+            if (n <= most) break;
+          }
+        }
+        return low;
+      };
+      uint64_t bound = (uint64_t)halve([](uint64_t key, uint32_t v) { return (uint32_t)(key >> 32) >= v; }) << 32;
+      if (count > most) bound |= halve([=](uint64_t key, uint32_t p) { return key >= (bound | p); });  // among equal values
+      if (tid == 0) lds.bound = bound;
+    }
+  } else if (tid < groups) {
     const uint64_t mine = lds.group[tid];
     int rank = 0;
 #pragma unroll 16
@@ -368,7 +403,7 @@ __global__ __launch_bounds__(64 * W, TOP && W < 16 ? 6 : 1) void logprobs_kernel
     else g.part_sums[block] = sums;
   }
   if constexpr (TOP) {
-    const uint64_t best = high_at < 0 ? 0 : key_of(high, high_at), bound = top_bound<W>(g.top, best, top);
+    const uint64_t best = high_at < 0 ? 0 : key_of(high, high_at), bound = top_bound<W>(g.top, best, top, whole && g.top > kTopShort);
     auto search = [&](const Wide<T>& y, int start) {
       if (key_of(largest<T>(y), start) < bound) return;
 #pragma unroll
@@ -378,12 +413,19 @@ __global__ __launch_bounds__(64 * W, TOP && W < 16 ? 6 : 1) void logprobs_kernel
     const bool mine = best && best >= bound;
     bool complete = true;
     if (mine && has_edge && key_of(edge, edge_at) >= bound) top_push(top, key_of(edge, edge_at));
-    if (!NOTES || batches <= 1) {
+    if (batches <= 1) {
       if (mine) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u)
           if (v0 + (int)threadIdx.x + u * NT < v1) search(x[u], cut.start(v0 + threadIdx.x + u * NT));
       }
+    } else if constexpr (!NOTES) {
+      if (mine)
+        for_batches<NT, false>(z, cut, v0, v1, [&](int i, const Packed<T>(&p)[kBatch]) {
+#pragma unroll
+          for (int u = 0; u < kBatch; ++u)
+            if (i + u * NT < v1) search(widen<T>(p[u]), cut.start(i + u * NT));
+        });
     } else {
       if (mine) {
         const float least = bound ? key_value(bound) : -__builtin_inff();
@@ -463,7 +505,7 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_join_kernel(LogprobArgs 
                                                 : row_sums(join_parts<false>(there, sums, Scale<false>{c}));
   if (threadIdx.x == 0) finish_logprobs(g, row, (float)z_token, token, r);
   if (!g.top) return;
-  const uint64_t bound = top_bound<kWaves>(g.top, best, top);
+  const uint64_t bound = top_bound<kWaves>(g.top, best, top, false);
   if (best && best >= bound)
     for (int i = threadIdx.x; i < nkeys; i += NT)
       if (keys[i] && keys[i] >= bound) top_push(top, keys[i]);
@@ -997,6 +1039,16 @@ uint32_t bitmap_bytes(int64_t vocab, int n, bool rest) {
 // 15.7, binary32 17.6 and 14.9; one of 200000 binary32 23.0 and 13.8; 100 of them 25.3 and 27.5; one of 32768
 // 7.9 and 10.6).
 constexpr int64_t kFewRows = 256, kSplitRows = 48, kSplitVocab = 98304;
+// Short rows: up to one batch of 256 threads' vectors such a block is as fast for few rows as one of 1024 (us for one row
+// of 8000 bf16 with 5 alternatives 6.1 and 7.3; 200 rows of 3500 with 64 9.1 and 11.0).  One wavefront a row,
+// which waits for no other, is faster for up to 256 vectors (8192 rows of 1000 binary32 8.8, 256 threads 19.4; with 5
+// alternatives 15.0 and 33.9) and for longer ones where rows are many: with `each` rows a vector or more, 2 for
+// the sums (8192 x 8000 bf16 25.3 and 29.5, 2048 x 8000 10.0 and 9.6, 1024 x 8000 8.2 and 6.9), 4 with alternatives (8192 x 3500
+// with 20 31.0 and 51.3, 8192 x 8000 54.5 and 57.2, 2048 x 8000 21.8 and 21.1, 1024 x 3500 12.8 and 11.0).
+constexpr int64_t kOneBatch = kBatch * 64 * kWaves;
+bool one_wave(int64_t rows, int64_t vectors, int64_t each) {
+  return vectors <= 256 || (vectors <= kOneBatch && rows >= each * vectors);
+}
 int row_parts(int64_t rows, int64_t vocab) {
   if (rows > kSplitRows || vocab < kSplitVocab) return 1;
   int64_t parts = (kBlocksWanted + rows - 1) / rows;
@@ -1014,8 +1066,9 @@ hipError_t launch_logprobs(const LogprobArgs& g, int dtype, hipStream_t stream) 
       if (g.top) HVDX_LAUNCH((logprobs_kernel<T, W, true>), grid, threads, 0, stream, g);
       else HVDX_LAUNCH((logprobs_kernel<T, W, false>), grid, threads, 0, stream, g);
     };
-    if (g.vocab / RowTypes<T>::n <= kBatch * 64) run(integral_constant<int, 1>{});  // one batch of one wavefront
-    else if (g.parts == 1 && g.rows <= kFewRows) run(integral_constant<int, 16>{});
+    const int64_t vectors = g.vocab / RowTypes<T>::n;
+    if (g.top <= kTopShort && one_wave(g.rows, vectors, g.top ? 4 : 2)) run(integral_constant<int, 1>{});
+    else if (g.parts == 1 && g.rows <= kFewRows && vectors > kOneBatch) run(integral_constant<int, 16>{});
     else run(integral_constant<int, kWaves>{});
   });
   return hipGetLastError();
@@ -1038,6 +1091,13 @@ hipError_t launch_logprobs_grad(const LogprobGradArgs& args, int dtype, hipStrea
   return hipGetLastError();
 }
 
+// Rows in registers, W waves of NV vectors a thread: as above for short rows (us for 8192 rows of 3500 bf16 with 20
+// entries: one wave 32.0, four 57; 8192 of 8000 51.8 and 61, 2048 17.4 and 18.7, 1024 12.2 and 10.8; 200 of 8000 four 6.3,
+// sixteen 7.1), and half the waves with twice the vectors each where that takes all rows at once: more rows than
+// compute units hold two blocks for (1024 x 32000 8 waves 28.1, 4 waves 24.2; 512 14.6 and 16.2).  Twice the vectors
+// again is no gain (8192 x 15000: 4 waves 92, 2 waves 101).  Rows read twice are slower (8192 x 8000 70.7, 2048 x
+// 131072 259 where rows in registers take 221, 200 x 65536 18.4 and 14.7).
+constexpr int64_t kHeldRows = 2 * 256;
 int distill_parts(int64_t rows, int64_t vocab, int dtype, bool grad) {
   if (grad && vocab / (dtype == HVDX_FLOAT32 ? 4 : 8) <= kRowMost) return 1;
   return row_parts(rows, vocab);
@@ -1066,16 +1126,19 @@ hipError_t launch_distill(const DistillArgs& g, int dtype, hipStream_t stream) {
     using std::false_type;
     using std::true_type;
     if (g.parts > 1 || !g.grad) {
-      if (vectors <= 256) pass(integral_constant<int, 1>{}, false_type{});
-      else if (g.parts == 1 && g.rows <= kFewRows) pass(integral_constant<int, 16>{}, false_type{});
+      if (one_wave(g.rows, vectors, 2)) pass(integral_constant<int, 1>{}, false_type{});
+      else if (g.parts == 1 && g.rows <= kFewRows && vectors > kOneBatch) pass(integral_constant<int, 16>{}, false_type{});
       else pass(integral_constant<int, kWaves>{}, false_type{});
     } else if (vectors < 2) {  // there may be no vector on its boundary
       pass(integral_constant<int, 1>{}, true_type{});
     } else if (vectors <= 256) HVDX_ROW(1, 4);
-    else if (g.rows <= kFewRows && vectors <= 4096) HVDX_ROW(16, 4);
-    else if (g.rows <= kFewRows && vectors <= 8192) HVDX_ROW(16, 8);
+    else if (g.rows <= kFewRows && vectors > kOneBatch && vectors <= 4096) HVDX_ROW(16, 4);
+    else if (g.rows <= kFewRows && vectors > kOneBatch && vectors <= 8192) HVDX_ROW(16, 8);
+    else if (g.rows > kHeldRows && vectors <= 512) HVDX_ROW(1, 8);
+    else if (g.rows >= 2 * vectors && vectors <= 1024) HVDX_ROW(1, 16);
     else if (vectors <= 1024) HVDX_ROW(4, 4);
     else if (vectors <= 2048) HVDX_ROW(4, 8);
+    else if (g.rows > kHeldRows && vectors <= 4096) HVDX_ROW(4, 16);
     else if (vectors <= 4096) HVDX_ROW(8, 8);
     else if (vectors <= 8192) HVDX_ROW(8, 16);
     else if (vectors <= kRowMost) HVDX_ROW(16, 16);

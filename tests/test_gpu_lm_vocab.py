@@ -503,3 +503,26 @@ def test_timeline_names_the_operators():
     assert all(r["duration_us"] > 0 and r["count"] == 64000 for r in tl.records)
     names = {e["name"] for e in tl.chrome_trace()["traceEvents"]}
     assert "token log probabilities" in names
+
+
+@pytest.mark.parametrize("rows,vocab,top,dtype", [(1100, 2087, 20, torch.bfloat16), (1300, 1081, 32, torch.float32), (4100, 8001, 7, torch.float16),
+                                                  (700, 3500, 0, torch.bfloat16), (300, 2000, 64, torch.bfloat16), (20, 2000, 64, torch.float16),
+                                                  (20, 1000, 64, torch.float32), (700, 8000, 64, torch.bfloat16), (30, 8003, 33, torch.bfloat16),
+                                                  (300, 70, 64, torch.float32)])
+def test_short_rows(rows, vocab, top, dtype):
+    """A wavefront a row over several batches of its vectors, and many alternatives of short rows."""
+    z = logits(rows, vocab, dtype, rows, offset=1)
+    special_rows(z)
+    tokens = torch.arange(rows, device="cuda") * 7919 % vocab
+    check_logprobs(z, tokens, 0.8, top, f"short {rows}")
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(600, 3500, torch.bfloat16), (1100, 1081, torch.float32), (2100, 8003, torch.bfloat16), (600, 20000, torch.float16),
+                                              (600, 32767, torch.bfloat16), (20, 3500, torch.bfloat16), (20, 8001, torch.float16)])
+def test_distill_short_rows(rows, vocab, dtype):
+    z = logits(rows, vocab, dtype, rows, offset=1)
+    special_rows(z)
+    for rest in (True, False):
+        ids, t = alternatives(rows, vocab, 9, rows)
+        ids[:, 0], ids[:, 1] = vocab - 1, 0
+        check_distill(z, ids, t, 1.2, rest, f"short {rows}", in_place=True)
